@@ -1,0 +1,155 @@
+// What the two attention kernels share: the arguments, the plan that deals the
+// work to workgroups, and the joining of a row's parts.
+//
+// Work is counted in units (a fixed number of tokens of one group of rows and
+// one cache head) and laid out in one line: requests, of a request its cache
+// heads, of a head its groups, of a group its units.  Workgroup w of W takes
+// the units [w T / W, (w + 1) T / W) of T, whatever rows they belong to, so
+// all end together however long the rows are.  A group that lies in several
+// workgroups' shares is joined by the last of them to arrive: each leaves the
+// maximum, the sum and the weighted values of its part, in FP32.
+#pragma once
+
+#include "paged_common.h"
+
+namespace paged {
+
+constexpr int kMaxShares = 2048;  // workgroups of a launch; one ticket each
+constexpr float kLow = -1e30f;    // below every score: the maximum of nothing
+constexpr float kSlack = 8.0f;    // a maximum may be passed by this much (powers of 2) before it moves
+
+struct Group {
+    int row0, rows, request, len;  // len: the longest of its rows
+};
+
+struct AttendArgs {
+    const uint8_t *k, *v;
+    const float *ks, *vs;
+    int64_t page_stride, scale_stride;
+    int n_pages, lp, kv_heads;
+    const void *q;
+    int64_t q_row, q_head;
+    void *out;
+    float *lse;
+    const int *table;
+    int table_stride, table_width;
+    const int *row_starts, *row_lengths;
+    int n_rows, n_requests;
+    int heads, per;   // query heads, and those of a cache head
+    int parts;        // cuts of those `per` heads, each a "head" of the plan
+    float scale2;     // scale * log2(e): scores are powers of 2
+    // the plan
+    int rows_per_group, max_groups, shares, unit;
+    int *tickets;     // [kMaxShares], zero between calls
+    Group *groups;    // [max_groups]
+    int *group_units; // [max_groups + 1] prefix sum of the groups' units
+    int *group_base;  // [n_requests + 1] first group of each request
+    int4 *starts;     // [shares] group, head, unit, request at a share's start
+    int64_t *total;   // [2] units in all, shares in use
+    float *left;      // [2 * shares] parts: per column maximum, sum, then values
+    // selected rows
+    const int *idx, *row_request;
+    int K, splits;
+};
+
+__device__ inline int64_t share_start(int64_t w, int64_t total, int64_t shares) { return w * total / shares; }
+__device__ inline int share_of(int64_t unit, int64_t total, int64_t shares) {
+    return (int)(((unit + 1) * shares - 1) / total);
+}
+
+// Parts go from one workgroup to another in relaxed agent-scope accesses, which
+// pass the XCDs' own caches; a wait for them, then the ticket, orders them.  (A
+// fence instead writes the whole L2 back: 300 us instead of 60 for one row of
+// 131071 tokens.)
+__device__ inline void give(float *p, float a, float b) {
+    __hip_atomic_store((uint64_t *)p, __builtin_bit_cast(uint64_t, f32x2{a, b}), __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline void give4(float *p, f32x4 x) {
+    give(p, x[0], x[1]);
+    give(p + 2, x[2], x[3]);
+}
+__device__ inline f32x2 taken(const float *p) {
+    return __builtin_bit_cast(
+        f32x2, __hip_atomic_load((const uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+__device__ inline f32x4 taken4(const float *p) {
+    const f32x2 a = taken(p), b = taken(p + 2);
+    return f32x4{a[0], a[1], b[0], b[1]};
+}
+// After the workgroup's stores of its part: is it the last of `parts` to arrive?
+// The ticket is back at 0 then.
+__device__ inline bool arrived_last(int *ticket, int parts, int *flag) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const int n = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (n == parts - 1) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *flag = n == parts - 1;
+    }
+    __syncthreads();
+    return *flag != 0;
+}
+
+// Columns [0, kCols) of a finished or partial group, in LDS: red[col][D + 4] the
+// weighted values, top and sum the softmax's.  Column c is row row0 + c / cols_per_row ...
+// `Place` says where a column's output goes: the element offset, or -1.
+template <int D, int COLS, int BLOCK, class T, class Place>
+__device__ void finish(const AttendArgs &a, float (*red)[D + 4], float *top, float *sum, bool whole, int slot,
+                       int first_share, int parts, int first_slot, Place place) {
+    __shared__ int last;
+    const int tid = threadIdx.x;
+    constexpr int kPart = COLS * (D + 2);
+    if (!whole) {
+        // a part: pairs of maximum and sum, then the values
+        float *mine = a.left + (int64_t)slot * kPart;
+        for (int i = tid; i < COLS * (D / 4); i += BLOCK) {
+            const int c = i / (D / 4), d = i % (D / 4) * 4;
+            give4(mine + 2 * COLS + c * D + d, *(const f32x4 *)&red[c][d]);
+        }
+        for (int c = tid; c < COLS; c += BLOCK) give(mine + 2 * c, top[c], sum[c]);
+        if (!arrived_last(&a.tickets[first_share], parts, &last)) return;
+        // part p lies in slot 0 of share first_share + p, the first one in first_slot
+        const auto part = [&](int p) {
+            return a.left + (int64_t)(p == 0 ? first_slot : 2 * (first_share + p)) * kPart;
+        };
+        for (int c = tid; c < COLS; c += BLOCK) {
+            float m = kLow, l = 0.0f;
+            for (int p = 0; p < parts; ++p) {
+                const f32x2 x = taken(part(p) + 2 * c);
+                const float to = fmaxf(m, x[0]);
+                l = l * exp2_(m - to) + x[1] * exp2_(x[0] - to);
+                m = to;
+            }
+            top[c] = m;
+            sum[c] = l;
+        }
+        __syncthreads();
+        for (int i = tid; i < COLS * (D / 4); i += BLOCK) {
+            const int c = i / (D / 4), d = i % (D / 4) * 4;
+            f32x4 o = {0, 0, 0, 0};
+            for (int p = 0; p < parts; ++p) {
+                const float *q = part(p);
+                o += taken4(q + 2 * COLS + c * D + d) * exp2_(taken(q + 2 * c)[0] - top[c]);
+            }
+            *(f32x4 *)&red[c][d] = o;
+        }
+        __syncthreads();
+    }
+    for (int i = tid; i < COLS * (D / 4); i += BLOCK) {
+        const int c = i / (D / 4), d = i % (D / 4) * 4;
+        const int64_t at = place(c);
+        if (at < 0) continue;
+        const float l = sum[c], inv = l != 0.0f ? 1.0f / l : 0.0f;
+        const f32x4 o = *(const f32x4 *)&red[c][d] * inv;
+        *(u32x2 *)((uint16_t *)a.out + at * D + d) = u32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
+        if (d == 0 && a.lse)
+            a.lse[at] = l != 0.0f ? (top[c] + __log2f(l)) * 0.6931471805599453f : -__builtin_inff();
+    }
+    __syncthreads();
+}
+
+int launch_stream(const AttendArgs &a, int head_dim, int act, int code, bool selected, int tiles, int grid, void *stream);
+int launch_prompt(const AttendArgs &a, int head_dim, int act, int code, int grid, void *stream);
+
+}  // namespace paged

@@ -1,0 +1,338 @@
+// Attention of many query rows to a cache head: prompts and chunks of them.
+//
+// Bound by the matrix products (4 D operations a pair of row and token) and by
+// the vector work of the softmax beside them.  A workgroup holds COLS columns
+// (rows x query heads of one cache head), 32 to a wave, their Q in registers;
+// tiles of 64 tokens go through LDS once for all waves, already as 16-bit
+// floats, while the next tile's codes are on their way from memory:
+//   S^T [token][col]  = K Q^T        O^T [dim][col] += V^T P^T
+// as 32 x 32 x 16 products.  The accumulator of S^T is the operand of P^T when
+// V's tokens are laid out in its order, so P never leaves its registers; V is
+// transposed on its way into LDS, by bytes.
+#include "paged_attend.h"
+
+namespace paged {
+namespace {
+
+constexpr int kTile = 64;
+
+// Chunk of 16 bytes of V's row d that holds chunk c: reads of 32 rows and writes
+// of every fourth row both spread over the banks.
+__device__ inline int swizzled(int d, int c) { return c ^ (((d >> 1) & 7) ^ ((d >> 4) & 1)); }
+
+template <int D, int WAVES>
+struct Buffers {
+    alignas(16) uint8_t k[kTile][2 * D + 16];
+    alignas(16) uint8_t v[D][2 * kTile];
+    float kf[4], vf[4];  // of each 16 tokens
+    u32 valid;           // bit of each 16 tokens: its page is in the cache
+};
+
+template <int D, int WAVES, class T, class C>
+__global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
+    constexpr int THREADS = 64 * WAVES, COLS = 32 * WAVES, PART = COLS * (D + 2);
+    constexpr int KI = kTile * D / 16, KN = (KI + THREADS - 1) / THREADS;  // 16-byte pieces of K, and of a thread
+    constexpr int VI = (kTile / 4) * (D / 4), VN = (VI + THREADS - 1) / THREADS;  // 4 x 4 pieces of V
+    __shared__ Buffers<D, WAVES> buf[2];
+    __shared__ int last;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, g = lane >> 5;
+    const int P = 1 << a.lp;
+    const int64_t total = a.total[0], shares = a.total[1];
+
+    // rows that no request has
+    for (int64_t i = max(a.row_starts[a.n_requests], 0) + (int64_t)blockIdx.x; i < a.n_rows; i += gridDim.x) {
+        for (int e = tid; e < a.heads * D / 2; e += THREADS) ((u32 *)a.out)[i * a.heads * D / 2 + e] = 0;
+        if (a.lse)
+            for (int e = tid; e < a.heads; e += THREADS) a.lse[i * a.heads + e] = -__builtin_inff();
+    }
+    if ((int)blockIdx.x >= shares) return;
+
+    const int share = blockIdx.x;
+    const int64_t begin = share_start(share, total, shares);
+    int64_t left = share_start(share + 1, total, shares) - begin;
+    const int4 st = a.starts[share];
+    int gi = st.x, head = st.y, unit = st.z, r = st.w;
+    const int vheads = a.kv_heads * a.parts;
+    const int per_row = min(a.per, COLS);  // columns of a row
+    while (left > 0) {
+        const Group gr = a.groups[gi];
+        const int units = a.group_units[gi + 1] - a.group_units[gi];
+        const int end = (int)min((int64_t)units, unit + left);
+        const int kvh = head / a.parts, part = head - kvh * a.parts;
+        const int *pages = a.table + (int64_t)gr.request * a.table_stride;
+
+        // this lane's column
+        const int col = 32 * wave + n, crow = col / per_row, chead = part * COLS + (col - crow * per_row);
+        const bool on = crow < gr.rows && chead < a.per;
+        const int64_t out_at = on ? (int64_t)(gr.row0 + crow) * a.heads + kvh * a.per + chead : -1;
+        const int len = on ? min(a.row_lengths[gr.row0 + crow], gr.len) : 0;
+        typename Act<T>::frag q[D / 16];
+        {
+            const char *p = (const char *)a.q + 2 * ((int64_t)(gr.row0 + crow) * a.q_row +
+                                                     (int64_t)(kvh * a.per + chead) * a.q_head);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                u32x4 x = {0, 0, 0, 0};
+                if (on) x = *(const u32x4 *)(p + 2 * (16 * k + 8 * g));
+                q[k] = __builtin_bit_cast(typename Act<T>::frag, x);
+            }
+        }
+        int shortest = on ? len : 0x7FFFFFFF, longest = len;
+        for (int d = 16; d; d >>= 1) {
+            shortest = min(shortest, __shfl_xor(shortest, d));
+            longest = max(longest, __shfl_xor(longest, d));
+        }
+        shortest = __builtin_amdgcn_readfirstlane(shortest);
+        longest = __builtin_amdgcn_readfirstlane(longest);
+
+        f32x16 o[D / 32];
+        for (int t = 0; t < D / 32; ++t)
+            for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
+        float m = kLow, l = 0.0f, ref = 0.0f, inv = 0.0f;
+
+        // codes on their way: pages a tile ahead of codes, codes a tile ahead of use
+        int kpage[KN], vpage[VN], spage = -1;
+        u32x4 kc[KN];
+        u32 vc[VN][4];
+        float sc = 0.0f;
+        const auto page_of = [&](int tok) {
+            if (tok >= gr.len) return -1;
+            const int pg = pages[tok >> a.lp];
+            return pg >= 0 && pg < a.n_pages ? pg : -1;
+        };
+        const auto look_up = [&](int u) {
+#pragma unroll
+            for (int e = 0; e < KN; ++e) kpage[e] = page_of(kTile * u + (tid + e * THREADS) / (D / 16));
+#pragma unroll
+            for (int e = 0; e < VN; ++e) vpage[e] = page_of(kTile * u + (tid + e * THREADS) / (D / 4) * 4);
+            if (tid < 8) spage = page_of(kTile * u + 16 * (tid & 3));
+        };
+        const auto fetch = [&](int u) {
+#pragma unroll
+            for (int e = 0; e < KN; ++e) {
+                const int i = tid + e * THREADS;
+                if (KI % THREADS != 0 && i >= KI) break;
+                const int tok = kTile * u + i / (D / 16);
+                const uint8_t *p = a.k + max(kpage[e], 0) * a.page_stride +
+                                   ((int64_t)kvh * P + (tok & (P - 1))) * D + i % (D / 16) * 16;
+                kc[e] = *(const u32x4 *)p;
+            }
+#pragma unroll
+            for (int e = 0; e < VN; ++e) {
+                const int i = tid + e * THREADS;
+                if (VI % THREADS != 0 && i >= VI) break;
+                const int tok = kTile * u + i / (D / 4) * 4;
+                const uint8_t *p = a.v + max(vpage[e], 0) * a.page_stride +
+                                   ((int64_t)kvh * P + (tok & (P - 1))) * D + i % (D / 4) * 4;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const u32 x = *(const u32 *)(p + j * D);
+                    // what is not there is 0 whatever its bytes are
+                    vc[e][j] = vpage[e] >= 0 && tok + j < gr.len ? x : 0u;
+                }
+            }
+            if (tid < 8) {
+                sc = 0.0f;
+                if (spage >= 0)
+                    sc = tid < 4 ? a.ks[spage * a.scale_stride + kvh] * a.scale2 : a.vs[spage * a.scale_stride + kvh];
+            }
+        };
+        const auto lay_out = [&](Buffers<D, WAVES> &b, int spage_of) {
+#pragma unroll
+            for (int e = 0; e < KN; ++e) {
+                const int i = tid + e * THREADS;
+                if (KI % THREADS != 0 && i >= KI) break;
+                u32x4 *to = (u32x4 *)&b.k[i / (D / 16)][i % (D / 16) * 32];
+                const u32x2 x0 = Four<C, T>::of(kc[e][0]), x1 = Four<C, T>::of(kc[e][1]);
+                const u32x2 x2 = Four<C, T>::of(kc[e][2]), x3 = Four<C, T>::of(kc[e][3]);
+                to[0] = u32x4{x0[0], x0[1], x1[0], x1[1]};
+                to[1] = u32x4{x2[0], x2[1], x3[0], x3[1]};
+            }
+#pragma unroll
+            for (int e = 0; e < VN; ++e) {
+                const int i = tid + e * THREADS;
+                if (VI % THREADS != 0 && i >= VI) break;
+                const int quad = i / (D / 4), d = i % (D / 4) * 4;
+                // tokens 16 s + 8 half + 4 g + j of 32 lie at 16 s + 8 g + 4 half + j
+                const int chunk = (quad >> 2) * 2 + (quad & 1), half = (quad >> 1) & 1;
+                u32 x[4];
+                transpose4(vc[e][0], vc[e][1], vc[e][2], vc[e][3], x);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *(u32x2 *)&b.v[d + j][16 * swizzled(d + j, chunk) + 8 * half] = Four<C, f16>::of(x[j]);
+            }
+            if (tid < 4) b.kf[tid] = sc;
+            else if (tid < 8) b.vf[tid - 4] = sc;
+            const u32 there = (u32)__ballot(tid < 4 && spage_of >= 0);
+            if (tid == 0) b.valid = there;
+        };
+
+        if (unit < end) {
+            look_up(unit);
+            fetch(unit);
+            int spage_now = spage;
+            if (unit + 1 < end) look_up(unit + 1);
+            lay_out(buf[0], spage_now);
+            __syncthreads();
+            for (int u = unit; u < end; ++u) {
+                const Buffers<D, WAVES> &b = buf[(u - unit) & 1];
+                if (u + 1 < end) {
+                    fetch(u + 1);
+                    spage_now = spage;
+                    if (u + 2 < end) look_up(u + 2);
+                }
+                const int tok0 = kTile * u;
+                if (tok0 < longest) {
+                    const f32x4 kf = *(const f32x4 *)b.kf;
+                    f32x4 vf = *(const f32x4 *)b.vf;
+                    const u32 valid = __builtin_amdgcn_readfirstlane(b.valid);
+                    const float vmax = fmaxf(fmaxf(vf[0], vf[1]), fmaxf(vf[2], vf[3]));
+                    if (__any(vmax > ref)) {
+                        const float to = 4.0f * vmax, by = ref / to;
+#pragma unroll
+                        for (int t = 0; t < D / 32; ++t) o[t] *= by;
+                        ref = to;
+                        inv = 1.0f / to;
+                    }
+                    vf *= inv;
+                    const bool all = valid == 15u && tok0 + kTile <= shortest;
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        f32x16 s;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k) {
+                            const u32x4 x = *(const u32x4 *)&b.k[32 * t + n][32 * k + 16 * g];
+                            s = Act<T>::mfma32(__builtin_bit_cast(typename Act<T>::frag, x), q[k], s);
+                        }
+                        float top = kLow;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            s[i] *= kf[2 * t + (i >> 3)];
+                            if (!all) {
+                                const int tok = tok0 + 32 * t + 8 * (i >> 2) + 4 * g + (i & 3);
+                                if (tok >= len || !((valid >> (2 * t + (i >> 3))) & 1)) s[i] = -__builtin_inff();
+                            }
+                            top = fmaxf(top, s[i]);
+                        }
+                        if (__any(top > m + kSlack)) {
+                            top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), m);
+                            const float by = exp2_(m - top);
+                            l *= by;
+#pragma unroll
+                            for (int d = 0; d < D / 32; ++d) o[d] *= by;
+                            m = top;
+                        }
+                        u32x4 p[2];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float e0 = exp2_(s[8 * h + 2 * i] - m), e1 = exp2_(s[8 * h + 2 * i + 1] - m);
+                                l += e0 + e1;
+                                p[h][i] = pack_f16(e0 * vf[2 * t + h], e1 * vf[2 * t + h]);
+                            }
+#pragma unroll
+                        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const int vd = 32 * d + n;
+                                const u32x4 x = *(const u32x4 *)&b.v[vd][16 * swizzled(vd, 4 * t + 2 * h + g)];
+                                o[d] = Act<f16>::mfma32(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, p[h]), o[d]);
+                            }
+                    }
+                }
+                if (u + 1 < end) lay_out(buf[(u + 1 - unit) & 1], spage_now);
+                __syncthreads();
+            }
+        }
+        l += __shfl_xor(l, 32);
+
+        // who else has a part of this group
+        const int gb0 = a.group_base[r], gb1 = a.group_base[r + 1];
+        const int64_t ru = a.group_units[gb1] - a.group_units[gb0];
+        const int64_t at = (int64_t)a.group_units[gb0] * vheads + head * ru + (a.group_units[gi] - a.group_units[gb0]);
+        const int s0 = share_of(at, total, shares), s1 = share_of(at + units - 1, total, shares), parts = s1 - s0 + 1;
+        if (parts == 1) {
+            const float by = l != 0.0f ? ref / l : 0.0f;
+            if (out_at >= 0) {
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+                        *(u32x2 *)((uint16_t *)a.out + out_at * D + 32 * d + 8 * b + 4 * g) =
+                            u32x2{pack2<T>(o[d][4 * b] * by, o[d][4 * b + 1] * by),
+                                  pack2<T>(o[d][4 * b + 2] * by, o[d][4 * b + 3] * by)};
+                if (a.lse && g == 0)
+                    a.lse[out_at] = l != 0.0f ? (m + __log2f(l)) * 0.6931471805599453f : -__builtin_inff();
+            }
+        } else {
+            const int first_slot = 2 * s0 + (at == share_start(s0, total, shares) ? 0 : 1);
+            float *mine = a.left + (int64_t)(share == s0 ? first_slot : 2 * share) * PART;
+            if (g == 0) give(mine + 2 * col, m, l);
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    give4(mine + 2 * COLS + col * D + 32 * d + 8 * b + 4 * g,
+                          f32x4{o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]} * ref);
+            if (arrived_last(&a.tickets[s0], parts, &last)) {
+                const auto part_at = [&](int p) {
+                    return a.left + (int64_t)(p == 0 ? first_slot : 2 * (s0 + p)) * PART;
+                };
+                for (int i = tid; i < COLS * (D / 4); i += THREADS) {
+                    const int c = i / (D / 4), d = i % (D / 4) * 4;
+                    const int row = c / per_row, h = part * COLS + (c - row * per_row);
+                    if (row >= gr.rows || h >= a.per) continue;
+                    float top = kLow, sum = 0.0f;
+                    for (int p = 0; p < parts; ++p) top = fmaxf(top, taken(part_at(p) + 2 * c)[0]);
+                    f32x4 x = {0, 0, 0, 0};
+                    for (int p = 0; p < parts; ++p) {
+                        const float *y = part_at(p);
+                        const f32x2 of = taken(y + 2 * c);
+                        const float by = exp2_(of[0] - top);
+                        sum += of[1] * by;
+                        x += taken4(y + 2 * COLS + c * D + d) * by;
+                    }
+                    x *= sum != 0.0f ? 1.0f / sum : 0.0f;
+                    const int64_t to = (int64_t)(gr.row0 + row) * a.heads + kvh * a.per + h;
+                    *(u32x2 *)((uint16_t *)a.out + to * D + d) = u32x2{pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3])};
+                    if (a.lse && d == 0)
+                        a.lse[to] = sum != 0.0f ? (top + __log2f(sum)) * 0.6931471805599453f : -__builtin_inff();
+                }
+            }
+            __syncthreads();
+        }
+        left -= end - unit;
+        unit = 0;
+        if (left > 0) {
+            ++gi;
+            if (gi == gb1) {
+                if (++head < vheads) gi = gb0;
+                else head = 0;
+            }
+            if (head == 0 && gi == gb1) r = a.groups[gi].request;
+        }
+    }
+}
+
+template <int D, int WAVES>
+int launch_dim(const AttendArgs &a, int act, int code, int grid, void *stream) {
+    const dim3 g((unsigned)grid), b(64 * WAVES);
+    if (code == PAGED_KV_E4M3)
+        return act == PAGED_KV_BF16 ? launch(prompt_kernel<D, WAVES, bf16, E4M3>, g, b, stream, a)
+                                    : launch(prompt_kernel<D, WAVES, f16, E4M3>, g, b, stream, a);
+    return act == PAGED_KV_BF16 ? launch(prompt_kernel<D, WAVES, bf16, Int8>, g, b, stream, a)
+                                : launch(prompt_kernel<D, WAVES, f16, Int8>, g, b, stream, a);
+}
+
+}  // namespace
+
+int launch_prompt(const AttendArgs &a, int head_dim, int act, int code, int grid, void *stream) {
+    if (head_dim == 64) return launch_dim<64, 8>(a, act, code, grid, stream);
+    if (head_dim == 128) return launch_dim<128, 8>(a, act, code, grid, stream);
+    return launch_dim<256, 4>(a, act, code, grid, stream);
+}
+
+}  // namespace paged

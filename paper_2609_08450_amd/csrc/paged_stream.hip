@@ -1,0 +1,471 @@
+// Attention of few query rows to a cache head: single tokens (one row to a
+// request) and selected tokens (one row to a selection).
+//
+// Bound by memory: 2 D bytes a token and cache head, read once, straight into
+// registers.  A wave takes 32 tokens at a time; the query heads of a cache head
+// are the 16 columns of its matrix products:
+//   S^T [token][col]  = K Q^T       K rows as they lie: lane (m, g) reads 16-byte pieces g, g + 4, .. of token m
+//   O^T [dim][col]   += V^T P^T     lane (m, g) reads D/16 bytes at m D/16 of the tokens 4 g + i, i < 4
+// The accumulator of S^T holds tokens 4 g + i of column m in lane (m, g), which
+// is just the operand layout of P^T with the tokens in the order (i, g); V's
+// bytes are brought to it by 4 x 4 byte transposes.  No value crosses lanes
+// but the maximum, and that only when it moves by more than 2^8.
+// P is rounded to f16 (11 bits, whatever q's type: V's codes are exact in it),
+// weighted with V's scale over the largest one seen so far, so that its range
+// does not depend on the scales.
+#include "paged_attend.h"
+
+namespace paged {
+namespace {
+
+constexpr int kBlock = 256;
+constexpr int kUnit = 128;     // tokens: 32 to a wave
+constexpr int kList = 1024;    // selected tokens looked up at a time
+
+// 32 tokens' codes of one lane.
+template <int D>
+struct Tile {
+    u32x4 k[2][D / 64];
+    u32 v[2][4][D / 64];
+};
+
+template <int D>
+__device__ void load_v(u32 (&to)[D / 64], const uint8_t *p) {
+    if constexpr (D == 64) {
+        to[0] = *(const u32 *)p;
+    } else if constexpr (D == 128) {
+        const u32x2 x = *(const u32x2 *)p;
+        to[0] = x[0]; to[1] = x[1];
+    } else {
+        const u32x4 x = *(const u32x4 *)p;
+        to[0] = x[0]; to[1] = x[1]; to[2] = x[2]; to[3] = x[3];
+    }
+}
+
+// One wave's running softmax and values for NT x 16 columns.
+template <int D, int NT, class T, class C>
+struct Wave {
+    typename Act<T>::frag q[NT][D / 32];
+    f32x4 o[NT][D / 16];
+    float m[NT], l[NT];
+    float ref, inv;  // values are held over `ref`
+
+    __device__ void clear() {
+        for (int t = 0; t < NT; ++t) {
+            m[t] = kLow;
+            l[t] = 0.0f;
+            for (int j = 0; j < D / 16; ++j) o[t][j] = f32x4{0, 0, 0, 0};
+        }
+        ref = 0.0f;
+        inv = 0.0f;
+    }
+
+    __device__ void reference(float vs) {  // wave-uniform
+        if (vs > ref) {
+            const float to = 4.0f * vs, by = ref / to;
+            for (int t = 0; t < NT; ++t)
+                for (int j = 0; j < D / 16; ++j) o[t][j] *= by;
+            ref = to;
+            inv = 1.0f / to;
+        }
+    }
+
+    // seen: bit 4 a + i says whether token 16 a + 4 g + i is there; kf, vf: scales
+    // of those tokens, the keys' times scale * log2(e), the values' over ref.
+    __device__ void take(const Tile<D> &x, u32 seen, bool all, const float (&kf)[2][4], const float (&vf)[2][4]) {
+        f32x4 s[NT][2];
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) s[t][a] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const auto kk = eight<C, T>(x.k[a][j][2 * h], x.k[a][j][2 * h + 1]);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) s[t][a] = Act<T>::mfma16(kk, q[t][2 * j + h], s[t][a]);
+                }
+        }
+        u32x4 p[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            float top = kLow;
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[t][a][i] *= kf[a][i];
+                    if (!all && !((seen >> (4 * a + i)) & 1)) s[t][a][i] = -__builtin_inff();
+                    top = fmaxf(top, s[t][a][i]);
+                }
+            if (__any(top > m[t] + kSlack)) {
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                top = fmaxf(top, m[t]);
+                const float by = exp2_(m[t] - top);
+                l[t] *= by;
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) o[t][j] *= by;
+                m[t] = top;
+            }
+            float e[2][4];
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    e[a][i] = exp2_(s[t][a][i] - m[t]);
+                    l[t] += e[a][i];
+                    e[a][i] *= vf[a][i];
+                }
+            p[t] = u32x4{pack_f16(e[0][0], e[0][1]), pack_f16(e[0][2], e[0][3]), pack_f16(e[1][0], e[1][1]),
+                         pack_f16(e[1][2], e[1][3])};
+        }
+#pragma unroll
+        for (int w = 0; w < D / 64; ++w) {
+            u32 r[2][4], c[2][4];
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)  // what is not there is 0 whatever its bytes are
+                    r[a][i] = all || ((seen >> (4 * a + i)) & 1) ? x.v[a][i][w] : 0u;
+                transpose4(r[a][0], r[a][1], r[a][2], r[a][3], c[a]);
+            }
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const auto vv = eight<C, f16>(c[0][b], c[1][b]);
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    o[t][4 * w + b] = Act<f16>::mfma16(vv, __builtin_bit_cast(f16x8, p[t]), o[t][4 * w + b]);
+            }
+        }
+    }
+};
+
+template <int D, int NT>
+struct Shared {
+    float red[16 * NT][D + 4];
+    float top[4][16 * NT], sum[4][16 * NT];
+    float tops[16 * NT], sums[16 * NT];
+};
+
+// The four waves' results into sh.red, sh.tops and sh.sums.
+template <int D, int NT, class T, class C>
+__device__ void join_waves(Wave<D, NT, T, C> &w, Shared<D, NT> &sh) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        float l = w.l[t];
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (g == 0) {
+            sh.top[wave][16 * t + n] = w.m[t];
+            sh.sum[wave][16 * t + n] = l;
+        }
+    }
+    __syncthreads();
+    float by[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int c = 16 * t + n;
+        float m = sh.top[0][c];
+        for (int i = 1; i < 4; ++i) m = fmaxf(m, sh.top[i][c]);
+        by[t] = exp2_(w.m[t] - m) * w.ref;
+        if (wave == 0 && g == 0) {
+            float l = 0.0f;
+            for (int i = 0; i < 4; ++i) l += sh.sum[i][c] * exp2_(sh.top[i][c] - m);
+            sh.tops[c] = m;
+            sh.sums[c] = l;
+        }
+    }
+    for (int turn = 0; turn < 4; ++turn) {
+        if (turn == wave) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < D / 16; j += 4) {
+                        f32x4 *to = (f32x4 *)&sh.red[16 * t + n][(4 * g + i) * (D / 16) + j];
+                        const f32x4 x = {w.o[t][j][i], w.o[t][j + 1][i], w.o[t][j + 2][i], w.o[t][j + 3][i]};
+                        *to = (turn ? *to : f32x4{0, 0, 0, 0}) + x * by[t];
+                    }
+        }
+        __syncthreads();
+    }
+}
+
+template <int D, int NT, class T, class C>
+__device__ void load_q(Wave<D, NT, T, C> &w, const AttendArgs &a, int row, int head0, int heads) {
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const bool on = 16 * t + n < heads;
+        const char *p = (const char *)a.q + 2 * ((int64_t)row * a.q_row + (int64_t)(head0 + 16 * t + n) * a.q_head);
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u32x4 x = {0, 0, 0, 0};
+                if (on) x = *(const u32x4 *)(p + 2 * ((g + 4 * j) * 16 + h * 8));
+                w.q[t][2 * j + h] = __builtin_bit_cast(typename Act<T>::frag, x);
+            }
+    }
+}
+
+// All tokens of single rows: the plan's groups have one row.
+template <int D, int NT, class T, class C>
+__global__ __launch_bounds__(kBlock) void stream_kernel(AttendArgs a) {
+    __shared__ Shared<D, NT> sh;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, g = lane >> 4;
+    const int P = 1 << a.lp;
+    const int64_t total = a.total[0], shares = a.total[1];
+
+    // rows that no request has
+    for (int64_t i = max(a.row_starts[a.n_requests], 0) + (int64_t)blockIdx.x; i < a.n_rows; i += gridDim.x) {
+        for (int e = tid; e < a.heads * D / 2; e += kBlock) ((u32 *)a.out)[i * a.heads * D / 2 + e] = 0;
+        if (a.lse)
+            for (int e = tid; e < a.heads; e += kBlock) a.lse[i * a.heads + e] = -__builtin_inff();
+    }
+    if ((int)blockIdx.x >= shares) return;
+
+    const int share = blockIdx.x;
+    const int64_t begin = share_start(share, total, shares);
+    int64_t left = share_start(share + 1, total, shares) - begin;
+    const int4 st = a.starts[share];
+    int gi = st.x, head = st.y, unit = st.z, r = st.w;
+    const int vheads = a.kv_heads * a.parts;
+    Wave<D, NT, T, C> w;
+    while (left > 0) {
+        const Group gr = a.groups[gi];
+        const int units = a.group_units[gi + 1] - a.group_units[gi];
+        const int end = (int)min((int64_t)units, unit + left);
+        const int kvh = head / a.parts, part = head - kvh * a.parts;
+        const int head0 = kvh * a.per + part * 16 * NT, heads = min(a.per - part * 16 * NT, 16 * NT);
+        w.clear();
+        load_q(w, a, gr.row0, head0, heads);
+
+        const int *pages = a.table + (int64_t)gr.request * a.table_stride;
+        const int64_t head_rows = (int64_t)kvh * P * D;
+        // tiles of this wave: 32 tokens at kUnit * u + 32 * wave
+        const int from = unit, stop = end;
+        int known = -1;  // block of 32 units whose pages the lanes hold: lane 2 i + a has unit i's half a
+        int page = -1;
+        float ks = 0.0f, vs = 0.0f;
+        const auto load = [&](Tile<D> &x, int u, int &lim0, int &lim1, float &k0, float &k1, float &v0, float &v1) {
+            const int blk = (u - from) >> 5;
+            if (blk != known) {
+                known = blk;
+                const int tok = kUnit * (from + 32 * blk + (lane >> 1)) + 32 * wave + 16 * (lane & 1);
+                page = -1;
+                ks = vs = 0.0f;
+                if (tok < gr.len) {
+                    const int pg = pages[tok >> a.lp];
+                    if (pg >= 0 && pg < a.n_pages) {
+                        page = pg;
+                        ks = a.ks[pg * a.scale_stride + kvh] * a.scale2;
+                        vs = a.vs[pg * a.scale_stride + kvh];
+                    }
+                }
+            }
+            const int i = 2 * ((u - from) & 31);
+            const int pg[2] = {__builtin_amdgcn_readlane(page, i), __builtin_amdgcn_readlane(page, i + 1)};
+            k0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), i));
+            k1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), i + 1));
+            v0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), i));
+            v1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), i + 1));
+            const int tok = kUnit * u + 32 * wave;
+            lim0 = pg[0] < 0 ? 0 : gr.len - tok;
+            lim1 = pg[1] < 0 ? 0 : gr.len - tok - 16;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t at = max(pg[h], 0) * a.page_stride + head_rows + ((tok + 16 * h) & (P - 1)) * D;
+                const uint8_t *kp = a.k + at, *vp = a.v + at;
+#pragma unroll
+                for (int j = 0; j < D / 64; ++j) x.k[h][j] = *(const u32x4 *)(kp + (u32)(m * D + g * 16 + 64 * j));
+#pragma unroll
+                for (int i2 = 0; i2 < 4; ++i2) load_v<D>(x.v[h][i2], vp + (u32)((4 * g + i2) * D + m * (D / 16)));
+            }
+        };
+        const auto take = [&](const Tile<D> &x, int lim0, int lim1, float k0, float k1, float v0, float v1) {
+            w.reference(fmaxf(v0, v1));
+            v0 *= w.inv;
+            v1 *= w.inv;
+            const float kf[2][4] = {{k0, k0, k0, k0}, {k1, k1, k1, k1}};
+            const float vf[2][4] = {{v0, v0, v0, v0}, {v1, v1, v1, v1}};
+            const bool all = lim0 >= 16 && lim1 >= 16;
+            u32 seen = 0xFF;
+            if (!all)
+                seen = ((1u << min(max(lim0 - 4 * g, 0), 4)) - 1) | (((1u << min(max(lim1 - 4 * g, 0), 4)) - 1) << 4);
+            if (all) w.take(x, 0xFF, true, kf, vf);
+            else if (lim0 > 0 || lim1 > 0) w.take(x, seen, false, kf, vf);
+        };
+        if (from < stop) {
+            Tile<D> x, y;
+            int xa, xb, ya, yb;
+            float xk0, xk1, xv0, xv1, yk0, yk1, yv0, yv1;
+            load(x, from, xa, xb, xk0, xk1, xv0, xv1);
+            for (int u = from; u < stop; u += 2) {
+                if (u + 1 < stop) load(y, u + 1, ya, yb, yk0, yk1, yv0, yv1);
+                take(x, xa, xb, xk0, xk1, xv0, xv1);
+                if (u + 1 >= stop) break;
+                if (u + 2 < stop) load(x, u + 2, xa, xb, xk0, xk1, xv0, xv1);
+                take(y, ya, yb, yk0, yk1, yv0, yv1);
+            }
+        }
+        join_waves(w, sh);
+        // who else has a part of this group
+        const int gb0 = a.group_base[r], gb1 = a.group_base[r + 1];
+        const int64_t ru = a.group_units[gb1] - a.group_units[gb0];
+        const int64_t at = (int64_t)a.group_units[gb0] * vheads + head * ru + (a.group_units[gi] - a.group_units[gb0]);
+        const int s0 = share_of(at, total, shares), s1 = share_of(at + units - 1, total, shares);
+        const int first_slot = 2 * s0 + (at == share_start(s0, total, shares) ? 0 : 1);
+        finish<D, 16 * NT, kBlock, T>(
+            a, sh.red, sh.tops, sh.sums, s0 == s1, share == s0 ? first_slot : 2 * share, s0, s1 - s0 + 1, first_slot,
+            [&](int c) { return c < heads ? (int64_t)gr.row0 * a.heads + head0 + c : (int64_t)-1; });
+        left -= end - unit;
+        unit = 0;
+        if (left > 0) {
+            ++gi;
+            if (gi == gb1) {
+                if (++head < vheads) gi = gb0;
+                else head = 0;
+            }
+            if (head == 0 && gi == gb1) r = a.groups[gi].request;
+        }
+    }
+}
+
+// The selected tokens of single rows: workgroup = (row, head, split).
+template <int D, int NT, class T, class C>
+__global__ __launch_bounds__(kBlock) void selected_kernel(AttendArgs a) {
+    __shared__ Shared<D, NT> sh;
+    __shared__ u32 rows[kList];  // head row of a token in the cache, or all ones
+    __shared__ float kf[kList], vf[kList];
+    __shared__ u32 vmax;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, g = lane >> 4;
+    const int P = 1 << a.lp, vheads = a.kv_heads * a.parts;
+    const int item = blockIdx.x / a.splits, split = blockIdx.x - item * a.splits;
+    const int row = item / vheads, head = item - row * vheads;
+    const int kvh = head / a.parts, part = head - kvh * a.parts;
+    const int head0 = kvh * a.per + part * 16 * NT, heads = min(a.per - part * 16 * NT, 16 * NT);
+    const int units = (a.K + kUnit - 1) / kUnit;
+    const int from = (int)((int64_t)units * split / a.splits) * kUnit;
+    const int stop = min((int)((int64_t)units * (split + 1) / a.splits) * kUnit, a.K);
+    const int request = a.row_request[row];
+    const bool known = request >= 0 && request < a.n_requests;
+    const int len = known ? min((int64_t)max(a.row_lengths[row], 0), (int64_t)a.table_width << a.lp) : 0;
+    const int *pages = a.table + (int64_t)(known ? request : 0) * a.table_stride;
+    const int *list = a.idx + (int64_t)row * a.K;
+    const u32 page_rows = (u32)(a.page_stride / D);
+
+    Wave<D, NT, T, C> w;
+    w.clear();
+    load_q(w, a, row, head0, heads);
+    for (int base = from; base < stop; base += kList) {
+        if (tid == 0) vmax = 0;
+        __syncthreads();
+        const int n = min(stop - base, kList), up = (n + kUnit - 1) / kUnit * kUnit;
+        float big = 0.0f;
+        for (int i = tid; i < up; i += kBlock) {
+            u32 at = ~0u;
+            float ks = 0.0f, vs = 0.0f;
+            const int t = i < n ? list[base + i] : -1;
+            if (t >= 0 && t < len) {
+                const int pg = pages[t >> a.lp];
+                if (pg >= 0 && pg < a.n_pages) {
+                    at = (u32)pg * page_rows + (u32)(kvh * P + (t & (P - 1)));
+                    ks = a.ks[pg * a.scale_stride + kvh] * a.scale2;
+                    vs = a.vs[pg * a.scale_stride + kvh];
+                }
+            }
+            rows[i] = at;
+            kf[i] = ks;
+            vf[i] = vs;
+            big = fmaxf(big, vs);
+        }
+        for (int d = 32; d; d >>= 1) big = fmaxf(big, __shfl_xor(big, d));
+        if (lane == 0 && big > 0.0f) atomicMax(&vmax, __float_as_uint(big));
+        __syncthreads();
+        w.reference(__uint_as_float(vmax));
+        const auto load = [&](Tile<D> &x, int i) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const u32 kr = rows[i + 16 * h + m];
+                const uint8_t *kp = a.k + (uint64_t)(kr == ~0u ? 0u : kr) * D;
+#pragma unroll
+                for (int j = 0; j < D / 64; ++j) x.k[h][j] = *(const u32x4 *)(kp + g * 16 + 64 * j);
+                const u32x4 vr = *(const u32x4 *)&rows[i + 16 * h + 4 * g];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    load_v<D>(x.v[h][e], a.v + (uint64_t)(vr[e] == ~0u ? 0u : vr[e]) * D + m * (D / 16));
+            }
+        };
+        const auto take = [&](const Tile<D> &x, int i) {
+            u32 seen = 0;
+            float k2[2][4], v2[2][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int at = i + 16 * h + 4 * g;
+                const u32x4 r = *(const u32x4 *)&rows[at];
+                const f32x4 ks = *(const f32x4 *)&kf[at], vs = *(const f32x4 *)&vf[at];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    seen |= (r[e] != ~0u ? 1u : 0u) << (4 * h + e);
+                    k2[h][e] = ks[e];
+                    v2[h][e] = vs[e] * w.inv;
+                }
+            }
+            if (__all(seen == 0xFF)) w.take(x, 0xFF, true, k2, v2);
+            else if (__any(seen != 0)) w.take(x, seen, false, k2, v2);
+        };
+        const int last = up;
+        if (32 * wave < last) {
+            Tile<D> x, y;
+            load(x, 32 * wave);
+            for (int i = 32 * wave; i < last; i += 2 * kUnit) {
+                if (i + kUnit < last) load(y, i + kUnit);
+                take(x, i);
+                if (i + kUnit >= last) break;
+                if (i + 2 * kUnit < last) load(x, i + 2 * kUnit);
+                take(y, i + kUnit);
+            }
+        }
+        __syncthreads();
+    }
+    join_waves(w, sh);
+    // splits of an item have neighbouring workgroups: shares item * splits + split
+    const int s0 = item * a.splits;
+    finish<D, 16 * NT, kBlock, T>(a, sh.red, sh.tops, sh.sums, a.splits == 1, 2 * (s0 + split), s0, a.splits, 2 * s0,
+                                  [&](int c) { return c < heads ? (int64_t)row * a.heads + head0 + c : (int64_t)-1; });
+}
+
+template <int D, class T, class C>
+int launch_of(const AttendArgs &a, bool selected, int tiles, int grid, void *stream) {
+    const dim3 g((unsigned)grid), b(kBlock);
+    if (selected)
+        return tiles == 1 ? launch(selected_kernel<D, 1, T, C>, g, b, stream, a)
+                          : launch(selected_kernel<D, 2, T, C>, g, b, stream, a);
+    return tiles == 1 ? launch(stream_kernel<D, 1, T, C>, g, b, stream, a)
+                      : launch(stream_kernel<D, 2, T, C>, g, b, stream, a);
+}
+
+template <int D>
+int launch_dim(const AttendArgs &a, int act, int code, bool selected, int tiles, int grid, void *stream) {
+    if (code == PAGED_KV_E4M3)
+        return act == PAGED_KV_BF16 ? launch_of<D, bf16, E4M3>(a, selected, tiles, grid, stream)
+                                    : launch_of<D, f16, E4M3>(a, selected, tiles, grid, stream);
+    return act == PAGED_KV_BF16 ? launch_of<D, bf16, Int8>(a, selected, tiles, grid, stream)
+                                : launch_of<D, f16, Int8>(a, selected, tiles, grid, stream);
+}
+
+}  // namespace
+
+int launch_stream(const AttendArgs &a, int head_dim, int act, int code, bool selected, int tiles, int grid,
+                  void *stream) {
+    if (head_dim == 64) return launch_dim<64>(a, act, code, selected, tiles, grid, stream);
+    if (head_dim == 128) return launch_dim<128>(a, act, code, selected, tiles, grid, stream);
+    return launch_dim<256>(a, act, code, selected, tiles, grid, stream);
+}
+
+}  // namespace paged

@@ -1,0 +1,102 @@
+"""paged_kv_score against its definition in 64 bits."""
+import pytest
+import torch
+
+from tests.paged_util import Setup, scores
+
+pytestmark = pytest.mark.gpu
+
+
+def check(s, gap=3, where="", seed=0):
+    from paper_2609_08450_amd import paged
+
+    print("[case] score", where, "rows", s.n_rows, "heads", s.heads, "dim", s.dim, "page", s.page, s.k.dtype, s.act,
+          flush=True)
+    s.cuda()
+    w = (torch.randn((s.n_rows, s.heads), generator=torch.Generator().manual_seed(seed))).cuda()
+    cap = s.table.shape[1] * s.page
+    length = s.row_lengths.clamp(min=0, max=cap).long().cpu()
+    offsets = torch.cumsum(length + gap, 0) - length  # a gap before each row
+    total = int((length + gap).sum()) + gap
+    out = torch.full((total,), 77.0, device="cuda")
+    paged.score(s.cache(), s.q, w, s.table, s.row_request, s.row_lengths, s.scale, out, offsets.cuda())
+    torch.cuda.synchronize()
+    rows, bound = scores(s, w)
+    touched = torch.zeros(total, dtype=torch.bool)
+    # FP32 products of exact operands: one rounding for each of D products, H sums, and the scales
+    unit = (s.dim + s.heads + 8) * 2.0 ** -24
+    for i, (want, b) in enumerate(zip(rows, bound)):
+        if want is None:
+            continue
+        o = int(offsets[i])
+        got = out[o:o + len(want)].double()
+        touched[o:o + len(want)] = True
+        there = want > -torch.inf
+        assert bool((got[~there] == -torch.inf).all()), f"{where}: row {i}, absent pages"
+        off = (got - want)[there].abs()
+        assert bool((off <= unit * b[there]).all()), f"{where}: row {i} off by {float(off.max()):.3g}"
+    assert bool((out.cpu()[~touched] == 77.0).all()), f"{where}: written past a row"
+    return out, offsets
+
+
+@pytest.mark.parametrize("code", [torch.float8_e4m3fn, torch.int8], ids=str)
+@pytest.mark.parametrize("act", [torch.bfloat16, torch.float16], ids=str)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("heads", [1, 2, 3, 4, 7, 8, 16, 17, 32, 100])
+def test_single_tokens_and_prompts(code, act, dim, heads):
+    lens = [1, 31, 33, 257, 700, 0]
+    kw = dict(kv=1, heads=heads, dim=dim, code=code, act=act, values=False)
+    check(Setup(lens, [1] * 6, page=16, **kw), where="single")
+    check(Setup([300, 64, 1, 200], [300, 5, 1, 37], page=64, **kw), where="prompts")
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+def test_pages(page):
+    check(Setup([5000, 17], [1, 1], page=page, kv=1, heads=8, dim=64, values=False), where="page")
+    check(Setup([1000, 17], [129, 3], page=page, kv=1, heads=8, dim=64, values=False), where="page, prompt")
+
+
+def test_windows_of_rows_of_many_requests():
+    check(Setup([40 + i for i in range(60)], [1 + i % 5 for i in range(60)], page=16, kv=1, heads=4, dim=64, values=False),
+          where="requests in a window")
+
+
+def test_rows_that_see_nothing_and_absent_pages():
+    s = Setup([200, 90, 33, 64], [2, 3, 1, 2], page=16, kv=1, heads=8, dim=64, values=False,
+              seen=[0, 150, -4, 90, 12, 33, 64, 10 ** 6])
+    s.table[0, 3], s.table[1, 0], s.table[1, 2], s.table[2, 0] = -1, s.n_pages, 2 ** 31 - 1, -5
+    s.row_request[3], s.row_request[6] = -1, 4
+    check(s, where="absent")
+
+
+def test_offsets_past_32_bits():
+    """Rows whose scores lie past 2^31 elements, from keys past 2^32 bytes."""
+    from paper_2609_08450_amd import paged
+
+    s = Setup([300], [2], page=64, kv=1, heads=8, dim=64, values=False).cuda()
+    far = 2 ** 32 // (64 * 64) + 11
+    cache = paged.PagedCache(far + s.n_pages, 64, 1, 64, values=False)
+    cache.k[far:], cache.k_scale[far:] = s.k, s.ks
+    w = torch.ones((2, 8), device="cuda")
+    near = torch.zeros(1000, device="cuda")
+    paged.score(s.cache(), s.q, w, s.table, s.row_request, s.row_lengths, s.scale, near, torch.tensor([0, 400]).cuda())
+    out = torch.zeros(2 ** 31 + 2000, device="cuda")
+    paged.score(cache, s.q, w, torch.where(s.table >= 0, s.table + far, s.table), s.row_request, s.row_lengths, s.scale, out,
+                torch.tensor([2 ** 31, 2 ** 31 + 400]).cuda())
+    assert torch.equal(out[2 ** 31:2 ** 31 + 1000], near) and float(near.abs().sum()) > 0
+
+
+def test_refusals():
+    from paper_2609_08450_amd import paged
+
+    s = Setup([50], [1], kv=1, heads=4, dim=64, values=False).cuda()
+    w, out, at = torch.ones((1, 4), device="cuda"), torch.zeros(50, device="cuda"), torch.zeros(1, dtype=torch.int64).cuda()
+    args = [s.cache(), s.q, w, s.table, s.row_request, s.row_lengths, s.scale, out, at]
+    paged.score(*args)
+    for i, bad in ((1, s.q.float()), (2, w[:, :3]), (2, w.half()), (3, s.table.long()), (4, s.row_request.long()),
+                   (5, s.row_lengths[:0]), (7, out.half()), (8, at.int()), (0, paged.PagedCache(2, 16, 2, 64)),
+                   (0, paged.PagedCache(2, 16, 1, 256, values=False))):
+        a = list(args)
+        a[i] = bad
+        with pytest.raises(paged.PagedError):
+            paged.score(*a)
