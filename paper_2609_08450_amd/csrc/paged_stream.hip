@@ -215,7 +215,7 @@ __device__ void load_q(Wave<D, NT, T, C> &w, const AttendArgs &a, int row, int h
 
 // All tokens of single rows: the plan's groups have one row.
 template <int D, int NT, class T, class C>
-__global__ __launch_bounds__(kBlock) void stream_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kBlock, D * NT <= 128 ? 2 : 1) void stream_kernel(AttendArgs a) {
     __shared__ Shared<D, NT> sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, g = lane >> 4;
     const int P = 1 << a.lp;
@@ -338,7 +338,7 @@ __global__ __launch_bounds__(kBlock) void stream_kernel(AttendArgs a) {
 
 // The selected tokens of single rows: workgroup = (row, head, split).
 template <int D, int NT, class T, class C>
-__global__ __launch_bounds__(kBlock) void selected_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kBlock, D * NT <= 128 ? 2 : 1) void selected_kernel(AttendArgs a) {
     __shared__ Shared<D, NT> sh;
     __shared__ u32 rows[kList];  // head row of a token in the cache, or all ones
     __shared__ float kf[kList], vf[kList];
