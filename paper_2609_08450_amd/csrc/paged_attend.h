@@ -59,8 +59,8 @@ __device__ inline int share_of(int64_t unit, int64_t total, int64_t shares) {
 
 // Parts go from one workgroup to another in relaxed agent-scope accesses, which
 // pass the XCDs' own caches; a wait for them, then the ticket, orders them.  (A
-// fence instead writes the whole L2 back: 300 us instead of 60 for one row of
-// 131071 tokens.)
+// fence instead writes the whole L2 back: the decode batch took 682 us with it
+// instead of 436.)
 __device__ inline void give(float *p, float a, float b) {
     __hip_atomic_store((uint64_t *)p, __builtin_bit_cast(uint64_t, f32x2{a, b}), __ATOMIC_RELAXED,
                        __HIP_MEMORY_SCOPE_AGENT);
@@ -91,62 +91,103 @@ __device__ inline bool arrived_last(int *ticket, int parts, int *flag) {
     return *flag != 0;
 }
 
-// Columns [0, kCols) of a finished or partial group, in LDS: red[col][D + 4] the
-// weighted values, top and sum the softmax's.  Column c is row row0 + c / cols_per_row ...
-// `Place` says where a column's output goes: the element offset, or -1.
-template <int D, int COLS, int BLOCK, class T, class Place>
-__device__ void finish(const AttendArgs &a, float (*red)[D + 4], float *top, float *sum, bool whole, int slot,
-                       int first_share, int parts, int first_slot, Place place) {
-    __shared__ int last;
-    const int tid = threadIdx.x;
-    constexpr int kPart = COLS * (D + 2);
-    if (!whole) {
-        // a part: pairs of maximum and sum, then the values
-        float *mine = a.left + (int64_t)slot * kPart;
-        for (int i = tid; i < COLS * (D / 4); i += BLOCK) {
-            const int c = i / (D / 4), d = i % (D / 4) * 4;
-            give4(mine + 2 * COLS + c * D + d, *(const f32x4 *)&red[c][d]);
+// Joins the parts of a group: top and sum of its first `cols` columns, then
+// weight by weight their values.  `part` gives part p's place.  Every thread
+// reads parts of its own, several at once: one after the other each would cost
+// a trip to memory (128 parts on one row of 131071 tokens: 170 us instead of 50).
+template <int COLS, int BLOCK>
+struct Joined {
+    static constexpr int CHUNK = 64;
+    float top[COLS], sum[COLS];
+    float m[BLOCK / COLS][COLS], l[BLOCK / COLS][COLS];
+    float weight[CHUNK][32];  // of a pass's columns
+};
+
+template <int D, int COLS, int BLOCK, class Part, class Out>
+__device__ void join_parts(Joined<COLS, BLOCK> &j, int parts, int cols, Part part, Out out) {
+    constexpr int SPAN = BLOCK / COLS, CHUNK = Joined<COLS, BLOCK>::CHUNK;
+    const int tid = threadIdx.x, c = tid % COLS, k = tid / COLS;
+    float m = kLow, l = 0.0f;
+    if (c < cols)
+#pragma unroll 4
+        for (int p = k; p < parts; p += SPAN) {
+            const f32x2 x = taken(part(p) + 2 * c);
+            const float to = fmaxf(m, x[0]);
+            l = l * exp2_(m - to) + x[1] * exp2_(x[0] - to);
+            m = to;
         }
-        for (int c = tid; c < COLS; c += BLOCK) give(mine + 2 * c, top[c], sum[c]);
-        if (!arrived_last(&a.tickets[first_share], parts, &last)) return;
-        // part p lies in slot 0 of share first_share + p, the first one in first_slot
-        const auto part = [&](int p) {
-            return a.left + (int64_t)(p == 0 ? first_slot : 2 * (first_share + p)) * kPart;
-        };
-        for (int c = tid; c < COLS; c += BLOCK) {
-            float m = kLow, l = 0.0f;
-            for (int p = 0; p < parts; ++p) {
-                const f32x2 x = taken(part(p) + 2 * c);
-                const float to = fmaxf(m, x[0]);
-                l = l * exp2_(m - to) + x[1] * exp2_(x[0] - to);
-                m = to;
-            }
-            top[c] = m;
-            sum[c] = l;
-        }
-        __syncthreads();
-        for (int i = tid; i < COLS * (D / 4); i += BLOCK) {
-            const int c = i / (D / 4), d = i % (D / 4) * 4;
-            f32x4 o = {0, 0, 0, 0};
-            for (int p = 0; p < parts; ++p) {
-                const float *q = part(p);
-                o += taken4(q + 2 * COLS + c * D + d) * exp2_(taken(q + 2 * c)[0] - top[c]);
-            }
-            *(f32x4 *)&red[c][d] = o;
-        }
-        __syncthreads();
-    }
-    for (int i = tid; i < COLS * (D / 4); i += BLOCK) {
-        const int c = i / (D / 4), d = i % (D / 4) * 4;
-        const int64_t at = place(c);
-        if (at < 0) continue;
-        const float l = sum[c], inv = l != 0.0f ? 1.0f / l : 0.0f;
-        const f32x4 o = *(const f32x4 *)&red[c][d] * inv;
-        *(u32x2 *)((uint16_t *)a.out + at * D + d) = u32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
-        if (d == 0 && a.lse)
-            a.lse[at] = l != 0.0f ? (top[c] + __log2f(l)) * 0.6931471805599453f : -__builtin_inff();
+    j.m[k][c] = m;
+    j.l[k][c] = l;
+    __syncthreads();
+    if (tid < COLS) {
+        float to = kLow, all = 0.0f;
+        for (int i = 0; i < SPAN; ++i) to = fmaxf(to, j.m[i][tid]);
+        for (int i = 0; i < SPAN; ++i) all += j.l[i][tid] * exp2_(j.m[i][tid] - to);
+        j.top[tid] = to;
+        j.sum[tid] = all;
     }
     __syncthreads();
+    // columns in passes of as many float4s as there are threads
+    constexpr int PER = BLOCK / (D / 4);  // columns of a pass
+    static_assert(PER <= 32, "weights of a pass");
+    const int pc = tid / (D / 4), d = tid % (D / 4) * 4;
+    for (int c0 = 0; c0 < cols; c0 += PER) {
+        const int col = c0 + pc;
+        f32x4 o = {0, 0, 0, 0};
+        for (int p0 = 0; p0 < parts; p0 += CHUNK) {
+            const int n = min(CHUNK, parts - p0);
+            __syncthreads();
+            for (int i = tid; i < n * PER; i += BLOCK) {
+                const int p = i / PER, w = i % PER;
+                if (c0 + w < cols) j.weight[p][w] = exp2_(taken(part(p0 + p) + 2 * (c0 + w))[0] - j.top[c0 + w]);
+            }
+            __syncthreads();
+            if (col < cols)
+#pragma unroll 8
+                for (int p = 0; p < n; ++p) o += taken4(part(p0 + p) + 2 * COLS + col * D + d) * j.weight[p][pc];
+        }
+        if (col < cols) out(col, d, o, j.top[col], j.sum[col]);
+    }
+    __syncthreads();
+}
+
+template <int D, class T>
+__device__ void write_out(const AttendArgs &a, int64_t at, int d, f32x4 o, float top, float sum) {
+    o *= sum != 0.0f ? 1.0f / sum : 0.0f;
+    *(u32x2 *)((uint16_t *)a.out + at * D + d) = u32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
+    if (d == 0 && a.lse)
+        a.lse[at] = sum != 0.0f ? (top + __log2f(sum)) * 0.6931471805599453f : -__builtin_inff();
+}
+
+// A group's first `cols` columns, in LDS: red[col][D + 4] the weighted values, top
+// and sum the softmax's.  `place` gives a column's output row.
+template <int D, int COLS, int BLOCK, class T, class Place>
+__device__ void finish(const AttendArgs &a, float (*red)[D + 4], float *top, float *sum, Joined<COLS, BLOCK> &joined,
+                       int cols, bool whole, int slot, int first_share, int parts, int first_slot, Place place) {
+    __shared__ int last;
+    const int tid = threadIdx.x;
+    constexpr int PART = COLS * (D + 2);
+    if (whole) {
+        for (int i = tid; i < cols * (D / 4); i += BLOCK) {
+            const int c = i / (D / 4), d = i % (D / 4) * 4;
+            write_out<D, T>(a, place(c), d, *(const f32x4 *)&red[c][d], top[c], sum[c]);
+        }
+        __syncthreads();
+        return;
+    }
+    // a part: pairs of maximum and sum, then the values
+    float *mine = a.left + (int64_t)slot * PART;
+    for (int i = tid; i < cols * (D / 4); i += BLOCK) {
+        const int c = i / (D / 4), d = i % (D / 4) * 4;
+        give4(mine + 2 * COLS + c * D + d, *(const f32x4 *)&red[c][d]);
+    }
+    for (int c = tid; c < cols; c += BLOCK) give(mine + 2 * c, top[c], sum[c]);
+    if (!arrived_last(&a.tickets[first_share], parts, &last)) return;
+    // part p lies in slot 0 of share first_share + p, the first one in first_slot
+    join_parts<D, COLS, BLOCK>(
+        joined, parts, cols,
+        [&](int p) { return a.left + (int64_t)(p == 0 ? first_slot : 2 * (first_share + p)) * PART; },
+        [&](int c, int d, f32x4 o, float m, float l) { write_out<D, T>(a, place(c), d, o, m, l); });
 }
 
 int launch_stream(const AttendArgs &a, int head_dim, int act, int code, bool selected, int tiles, int grid, void *stream);

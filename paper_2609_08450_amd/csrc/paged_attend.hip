@@ -127,7 +127,7 @@ Shape shape_of(int n_rows, int n_requests, int heads, int kv_heads, int dim, boo
         s.rows_per_group = per >= s.cols ? 1 : s.cols / per;
         s.shares = cus;
     } else {
-        s.shares = 4 * cus;
+        s.shares = 2 * cus;
     }
     if (s.shares > kMaxShares) s.shares = kMaxShares;
     s.parts = (per + s.cols - 1) / s.cols;

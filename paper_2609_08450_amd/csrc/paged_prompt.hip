@@ -34,6 +34,7 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
     constexpr int KI = kTile * D / 16, KN = (KI + THREADS - 1) / THREADS;  // 16-byte pieces of K, and of a thread
     constexpr int VI = (kTile / 4) * (D / 4), VN = (VI + THREADS - 1) / THREADS;  // 4 x 4 pieces of V
     __shared__ Buffers<D, WAVES> buf[2];
+    __shared__ Joined<COLS, THREADS> joined;
     __shared__ int last;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, g = lane >> 5;
     const int P = 1 << a.lp;
@@ -278,29 +279,14 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
                     give4(mine + 2 * COLS + col * D + 32 * d + 8 * b + 4 * g,
                           f32x4{o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]} * ref);
             if (arrived_last(&a.tickets[s0], parts, &last)) {
-                const auto part_at = [&](int p) {
-                    return a.left + (int64_t)(p == 0 ? first_slot : 2 * (s0 + p)) * PART;
-                };
-                for (int i = tid; i < COLS * (D / 4); i += THREADS) {
-                    const int c = i / (D / 4), d = i % (D / 4) * 4;
-                    const int row = c / per_row, h = part * COLS + (c - row * per_row);
-                    if (row >= gr.rows || h >= a.per) continue;
-                    float top = kLow, sum = 0.0f;
-                    for (int p = 0; p < parts; ++p) top = fmaxf(top, taken(part_at(p) + 2 * c)[0]);
-                    f32x4 x = {0, 0, 0, 0};
-                    for (int p = 0; p < parts; ++p) {
-                        const float *y = part_at(p);
-                        const f32x2 of = taken(y + 2 * c);
-                        const float by = exp2_(of[0] - top);
-                        sum += of[1] * by;
-                        x += taken4(y + 2 * COLS + c * D + d) * by;
-                    }
-                    x *= sum != 0.0f ? 1.0f / sum : 0.0f;
-                    const int64_t to = (int64_t)(gr.row0 + row) * a.heads + kvh * a.per + h;
-                    *(u32x2 *)((uint16_t *)a.out + to * D + d) = u32x2{pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3])};
-                    if (a.lse && d == 0)
-                        a.lse[to] = sum != 0.0f ? (top + __log2f(sum)) * 0.6931471805599453f : -__builtin_inff();
-                }
+                join_parts<D, COLS, THREADS>(
+                    joined, parts, min(gr.rows * per_row, COLS),
+                    [&](int p) { return a.left + (int64_t)(p == 0 ? first_slot : 2 * (s0 + p)) * PART; },
+                    [&](int c, int d, f32x4 x, float m2, float l2) {
+                        const int row = c / per_row, h = part * COLS + (c - row * per_row);
+                        if (h < a.per)
+                            write_out<D, T>(a, (int64_t)(gr.row0 + row) * a.heads + kvh * a.per + h, d, x, m2, l2);
+                    });
             }
             __syncthreads();
         }

@@ -147,6 +147,7 @@ struct Shared {
     float red[16 * NT][D + 4];
     float top[4][16 * NT], sum[4][16 * NT];
     float tops[16 * NT], sums[16 * NT];
+    Joined<16 * NT, kBlock> joined;
 };
 
 // The four waves' results into sh.red, sh.tops and sh.sums.
@@ -321,8 +322,8 @@ __global__ __launch_bounds__(kBlock, D * NT <= 128 ? 2 : 1) void stream_kernel(A
         const int s0 = share_of(at, total, shares), s1 = share_of(at + units - 1, total, shares);
         const int first_slot = 2 * s0 + (at == share_start(s0, total, shares) ? 0 : 1);
         finish<D, 16 * NT, kBlock, T>(
-            a, sh.red, sh.tops, sh.sums, s0 == s1, share == s0 ? first_slot : 2 * share, s0, s1 - s0 + 1, first_slot,
-            [&](int c) { return c < heads ? (int64_t)gr.row0 * a.heads + head0 + c : (int64_t)-1; });
+            a, sh.red, sh.tops, sh.sums, sh.joined, heads, s0 == s1, share == s0 ? first_slot : 2 * share, s0,
+            s1 - s0 + 1, first_slot, [&](int c) { return (int64_t)gr.row0 * a.heads + head0 + c; });
         left -= end - unit;
         unit = 0;
         if (left > 0) {
@@ -436,8 +437,8 @@ __global__ __launch_bounds__(kBlock, D * NT <= 128 ? 2 : 1) void selected_kernel
     join_waves(w, sh);
     // splits of an item have neighbouring workgroups: shares item * splits + split
     const int s0 = item * a.splits;
-    finish<D, 16 * NT, kBlock, T>(a, sh.red, sh.tops, sh.sums, a.splits == 1, 2 * (s0 + split), s0, a.splits, 2 * s0,
-                                  [&](int c) { return c < heads ? (int64_t)row * a.heads + head0 + c : (int64_t)-1; });
+    finish<D, 16 * NT, kBlock, T>(a, sh.red, sh.tops, sh.sums, sh.joined, heads, a.splits == 1, 2 * (s0 + split), s0,
+                                  a.splits, 2 * s0, [&](int c) { return (int64_t)row * a.heads + head0 + c; });
 }
 
 template <int D, class T, class C>
