@@ -17,7 +17,6 @@ namespace paged {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kTiles = 4;  // products of 32 query rows x heads in LDS at a time
 
 // Tokens of a lane: what the registers hold beside the sums.
 constexpr int tokens_of(int dim, int hp) { return dim == 64 && hp >= 4 ? 4 : 2; }
@@ -77,38 +76,55 @@ __device__ typename Act<T>::frag query(const uint8_t *row, int step, int g) {
     return __builtin_bit_cast(typename Act<T>::frag, *(const u32x4 *)(row + 64 * (step >> 1) + 32 * g + 16 * (step & 1)));
 }
 
+// max(x, 0) as one instruction, on the bits: a float maximum makes a second one
+// of a result that the compiler cannot know to be no signalling NaN.
+__device__ inline float relu(float x) { return __int_as_float(max(__float_as_int(x), 0)); }
+
+// NT scores of a lane, past the caches: nothing reads them before the call ends.
 template <int NT>
-__device__ void put(float *to, const float (&x)[NT], float scale, int left) {
-    float y[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) y[t] = scale == -__builtin_inff() ? scale : x[t] * scale;
-    if (left >= NT) {
-        if constexpr (NT == 4) *(f32x4_any *)to = f32x4_any{y[0], y[1], y[2], y[3]};
-        else *(f32x2_any *)to = f32x2_any{y[0], y[1]};
-    } else {
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-            if (t < left) to[t] = y[t];
-    }
+__device__ void put_all(float *to, const float (&x)[NT], float scale) {
+    if constexpr (NT == 4)
+        __builtin_nontemporal_store(f32x4_any{x[0], x[1], x[2], x[3]} * scale, (f32x4_any *)to);
+    else
+        __builtin_nontemporal_store(f32x2_any{x[0], x[1]} * scale, (f32x2_any *)to);
 }
 
-// Windows of rows: workgroup = (4 waves x 32 NT tokens, `window` rows).
-template <int D, int HP, class T, class C>
-__global__ __launch_bounds__(kBlock, 2) void score_block_kernel(ScoreArgs a) {
-    constexpr int NT = tokens_of(D, HP);
-    typedef Rows<HP> R;
-    constexpr int PIECES = 32 * kTiles * D / 8 / kBlock;  // 16-byte pieces of queries that a thread stages
-    __shared__ alignas(16) uint8_t qs[32 * kTiles][2 * D + 16];
-    __shared__ alignas(16) float ws[kTiles][2][16];  // by half wave
-    __shared__ int64_t offs[kTiles][R::COUNT];
-    __shared__ int lens[kTiles][R::COUNT];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, g = lane >> 5;
-    const int chunks = (a.heads + HP - 1) / HP;  // more than one only where HP is 16
-    const int wave_tok = (int)blockIdx.x * (kBlock / 64 * 32 * NT) + 32 * NT * wave, tok = wave_tok + NT * n;
-    const int row_end = min((int)(blockIdx.y + 1) * a.window, a.n_rows);
-    const int64_t cap = (int64_t)a.table_width << a.lp;
+// The same for the first `left` of them; scale -inf stands for a page outside the cache.
+template <int NT>
+__device__ void put(float *to, const float (&x)[NT], float scale, int left) {
+    if (left >= NT && scale != -__builtin_inff()) return put_all<NT>(to, x, scale);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+        if (t < left) to[t] = scale == -__builtin_inff() ? scale : x[t] * scale;
+}
 
-    int row = blockIdx.y * a.window;
+// Query rows x heads that a workgroup holds, and query rows where every product
+// row is one (their lengths and places).
+constexpr int window_of(int dim) { return dim == 64 ? 512 : 256; }
+
+// Windows of rows: workgroup = (`window` rows, every gridDim.y-th of the blocks of
+// 4 waves x 32 NT tokens).  The queries stay in LDS, each wave passes its own
+// tokens by them: no barrier and no load of queries between the stores, whose
+// way to memory the next barrier would wait for (573 us without the stores, 795
+// with them and a barrier every four products).
+// MANY: more heads than a product holds (HP is 16 then).
+template <int D, int HP, bool MANY, class T, class C>
+__global__ __launch_bounds__(kBlock, 2) void score_block_kernel(ScoreArgs a) {
+    constexpr int NT = tokens_of(D, HP), M = window_of(D), STEP = kBlock / 64 * 32 * NT;
+    typedef Rows<HP> R;
+    __shared__ alignas(16) uint8_t qs[M][2 * D];  // 16-byte pieces in swizzled order
+    __shared__ alignas(16) float ws[M];           // product, half wave, place
+    __shared__ int64_t offs[M / HP];
+    __shared__ int lens[M / HP], longest[M / 32], shortest[M / 32];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, g = lane >> 5;
+    const int chunks = MANY ? (a.heads + HP - 1) / HP : 1;
+    const int64_t cap = (int64_t)a.table_width << a.lp;
+    // the last windows first: where lengths rise they are the longest
+    const int y = gridDim.x - 1 - blockIdx.x;
+    const int row_end = min((y + 1) * a.window, a.n_rows);
+    const auto place = [](int m, int piece) { return 16 * (piece ^ (D == 64 ? (m >> 1) & 7 : m & 15)); };
+
+    int row = y * a.window;
     while (row < row_end) {
         // the rows from here on that share their request
         const int request = a.row_request[row];
@@ -119,14 +135,55 @@ __global__ __launch_bounds__(kBlock, 2) void score_block_kernel(ScoreArgs a) {
             on = other == 0;
             stop += on ? 64 : __builtin_ctzll(other);
         }
-        const int first = row;
+        const int first = row, rows = stop - row;
         row = stop;
         if (request < 0 || request >= a.n_requests) continue;
-        typename Act<T>::frag k[NT][D / 16];
-        float scale;
-        {
-            Keys<D, NT> raw;
-            load_keys<D, NT>(raw, a, tok < cap ? a.table[(int64_t)request * a.table_stride + (tok >> a.lp)] : -1, tok, g);
+        const int products = (rows + R::COUNT - 1) / R::COUNT * chunks;  // product p: rows p / chunks, heads p % chunks
+        __syncthreads();  // the rows before these are done with
+        for (int i = tid; i < 32 * products * (D / 8); i += kBlock) {
+            const int m = i / (D / 8), piece = i % (D / 8), p = m / 32;
+            const int r = p / chunks * R::COUNT + R::row(m % 32), h = p % chunks * HP + R::head(m % 32);
+            u32x4 x = {0, 0, 0, 0};
+            if (r < rows && h < a.heads)
+                x = *(const u32x4 *)((const char *)a.q + 2 * ((first + r) * a.q_row + h * a.q_head + 8 * piece));
+            *(u32x4 *)&qs[m][place(m, piece)] = x;
+        }
+        for (int i = tid; i < 32 * products; i += kBlock) {
+            const int p = i / 32, at = i % 16;
+            const int r = p / chunks * R::COUNT + (i >> 4 & 1) * R::HALF + at / HP, h = p % chunks * HP + at % HP;
+            ws[i] = r < rows && h < a.heads ? a.w[(int64_t)(first + r) * a.heads + h] : 0.0f;
+        }
+        for (int i = tid; i < products / chunks * R::COUNT; i += kBlock) {
+            lens[i] = i < rows ? (int)min((int64_t)max(a.row_lengths[first + i], 0), cap) : 0;
+            offs[i] = i < rows ? a.row_offsets[first + i] : 0;
+        }
+        __syncthreads();
+        int top = 0;
+        for (int i = tid; i < products / chunks; i += kBlock) {
+            int x = 0, y = 0x7FFFFFFF;
+            for (int r = 0; r < R::COUNT; ++r) {
+                x = max(x, lens[i * R::COUNT + r]);
+                y = min(y, lens[i * R::COUNT + r]);
+            }
+            longest[i] = x;
+            shortest[i] = y;
+        }
+        __syncthreads();
+        for (int i = lane; i < products / chunks; i += 64) top = max(top, longest[i]);
+        for (int d = 32; d; d >>= 1) top = max(top, __shfl_xor(top, d));
+        top = __builtin_amdgcn_readfirstlane(top);
+
+        const int *pages = a.table + (int64_t)request * a.table_stride;
+        const int step = gridDim.y * STEP;
+        const auto page_of = [&](int tok) { return tok < top ? pages[tok >> a.lp] : -1; };
+        int base = blockIdx.y * STEP + 32 * NT * wave;
+        Keys<D, NT> raw;
+        int page = page_of(base + NT * n);
+        load_keys<D, NT>(raw, a, page, base + NT * n, g);
+        if (base < top) page = page_of((int)min((int64_t)base + step, (int64_t)0x7FFFFFFF - STEP) + NT * n);
+        while (base < top) {
+            const int tok = base + NT * n;
+            typename Act<T>::frag k[NT][D / 16];
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -134,51 +191,20 @@ __global__ __launch_bounds__(kBlock, 2) void score_block_kernel(ScoreArgs a) {
                     k[t][2 * j] = eight<C, T>(raw.x[t][j][0], raw.x[t][j][1]);
                     k[t][2 * j + 1] = eight<C, T>(raw.x[t][j][2], raw.x[t][j][3]);
                 }
-            scale = raw.scale;
-        }
-        const int products = (stop - first + R::COUNT - 1) / R::COUNT * chunks;  // product p: rows p / chunks, heads p % chunks
-        u32x4 staged[PIECES];
-        float staged_w = 0.0f;
-        int64_t staged_off = 0;
-        int staged_len = 0;
-        const auto fetch = [&](int p0) {
-#pragma unroll
-            for (int e = 0; e < PIECES; ++e) {
-                const int i = tid + e * kBlock, m = i / (D / 8), d = i % (D / 8) * 8, p = p0 + m / 32;
-                const int r = first + p / chunks * R::COUNT + R::row(m % 32), h = p % chunks * HP + R::head(m % 32);
-                staged[e] = u32x4{0, 0, 0, 0};
-                if (r < stop && h < a.heads)
-                    staged[e] = *(const u32x4 *)((const char *)a.q + 2 * (r * a.q_row + h * a.q_head + d));
+            const float scale = raw.scale;
+            const int next = (int)min((int64_t)base + step, (int64_t)0x7FFFFFFF - STEP);
+            if (next < top) {
+                load_keys<D, NT>(raw, a, page, next + NT * n, g);
+                page = page_of((int)min((int64_t)next + step, (int64_t)0x7FFFFFFF - STEP) + NT * n);
             }
-            if (tid < 32 * kTiles) {
-                const int half = (tid >> 4) & 1, place = tid & 15, p = p0 + tid / 32;
-                const int r = first + p / chunks * R::COUNT + half * R::HALF + place / HP, h = p % chunks * HP + place % HP;
-                staged_w = r < stop && h < a.heads ? a.w[(int64_t)r * a.heads + h] : 0.0f;
-            }
-            if (tid < kTiles * R::COUNT) {
-                const int r = first + (p0 + tid / R::COUNT) / chunks * R::COUNT + tid % R::COUNT;
-                staged_len = r < stop ? (int)min((int64_t)max(a.row_lengths[r], 0), cap) : 0;
-                staged_off = r < stop ? a.row_offsets[r] : 0;
-            }
-        };
-        fetch(0);
-        float sum[R::HALF][NT];
-        for (int p0 = 0; p0 < products; p0 += kTiles) {
-            __syncthreads();
-#pragma unroll
-            for (int e = 0; e < PIECES; ++e) {
-                const int i = tid + e * kBlock;
-                *(u32x4 *)&qs[i / (D / 8)][i % (D / 8) * 16] = staged[e];
-            }
-            if (tid < 32 * kTiles) ws[tid / 32][(tid >> 4) & 1][tid & 15] = staged_w;
-            if (tid < kTiles * R::COUNT) {
-                lens[tid / R::COUNT][tid % R::COUNT] = staged_len;
-                offs[tid / R::COUNT][tid % R::COUNT] = staged_off;
-            }
-            __syncthreads();
-            if (p0 + kTiles < products) fetch(p0 + kTiles);
-            for (int m = 0; m < kTiles && p0 + m < products; ++m) {
-                const int c = (p0 + m) % chunks;
+            const bool plain = __all(scale != -__builtin_inff());
+            float sum[R::HALF][NT];
+            int c = 0, group = 0;
+            for (int p = 0; p < products; ++p) {
+                if (base >= __builtin_amdgcn_readfirstlane(longest[group])) {  // no row of this product comes so far
+                    if (++c == chunks) c = 0, ++group;
+                    continue;
+                }
                 if (c == 0)
 #pragma unroll
                     for (int i = 0; i < R::HALF; ++i)
@@ -191,25 +217,33 @@ __global__ __launch_bounds__(kBlock, 2) void score_block_kernel(ScoreArgs a) {
                     for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
 #pragma unroll
                 for (int j = 0; j < D / 16; ++j) {
-                    const auto x = query<D, T>(qs[32 * m + n], j, g);
+                    const int m = 32 * p + n;
+                    const u32x4 x = *(const u32x4 *)&qs[m][place(m, 4 * (j >> 1) + 2 * g + (j & 1))];
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) s[t] = Act<T>::mfma32(x, k[t][j], s[t]);
+                    for (int t = 0; t < NT; ++t)
+                        s[t] = Act<T>::mfma32(__builtin_bit_cast(typename Act<T>::frag, x), k[t][j], s[t]);
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float w = ws[m][g][i];
+                    const float w = ws[32 * p + 16 * g + i];
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) sum[i / HP][t] = fmaf(w, fmaxf(s[t][i], 0.0f), sum[i / HP][t]);
+                    for (int t = 0; t < NT; ++t) sum[i / HP][t] = fmaf(w, relu(s[t][i]), sum[i / HP][t]);
                 }
-                if (c == chunks - 1)
+                if (++c == chunks) {
+                    const int r = group * R::COUNT + g * R::HALF;
+                    if (plain && base + 32 * NT <= __builtin_amdgcn_readfirstlane(shortest[group]))
 #pragma unroll
-                    for (int i = 0; i < R::HALF; ++i) {
-                        const int r = g * R::HALF + i;
-                        put<NT>(a.scores + offs[m][r] + tok, sum[i], scale, lens[m][r] - tok);
-                    }
+                        for (int i = 0; i < R::HALF; ++i) put_all<NT>(a.scores + offs[r + i] + tok, sum[i], scale);
+                    else
+#pragma unroll
+                        for (int i = 0; i < R::HALF; ++i)
+                            put<NT>(a.scores + offs[r + i] + tok, sum[i], scale, lens[r + i] - tok);
+                    c = 0;
+                    ++group;
+                }
             }
+            base = next;
         }
-        __syncthreads();
     }
 }
 
@@ -282,7 +316,7 @@ __global__ __launch_bounds__(kBlock, 2) void score_row_kernel(ScoreArgs a) {
             for (int i = 0; i < HP; ++i) {
                 const float w = ws[c * HP + i];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) sum[t] = fmaf(w, fmaxf(x[t][i], 0.0f), sum[t]);
+                for (int t = 0; t < NT; ++t) sum[t] = fmaf(w, relu(x[t][i]), sum[t]);
             }
         }
         if (g == 0) put<NT>(out + tile + NT * n, sum, now.scale, len - (tile + NT * n));
@@ -290,19 +324,17 @@ __global__ __launch_bounds__(kBlock, 2) void score_row_kernel(ScoreArgs a) {
     }
 }
 
-template <int D, int HP, class T, class C>
-int launch_rows(const ScoreArgs &a, dim3 grid, void *stream) {
-    return a.window == 1 ? launch(score_row_kernel<D, HP, T, C>, grid, dim3(kBlock), stream, a)
-                         : launch(score_block_kernel<D, HP, T, C>, grid, dim3(kBlock), stream, a);
-}
-
 template <int D, class T, class C>
 int launch_heads(const ScoreArgs &a, dim3 grid, void *stream) {
-    if (a.heads == 1) return launch_rows<D, 1, T, C>(a, grid, stream);
-    if (a.heads == 2) return launch_rows<D, 2, T, C>(a, grid, stream);
-    if (a.heads <= 4) return launch_rows<D, 4, T, C>(a, grid, stream);
-    if (a.heads <= 8) return launch_rows<D, 8, T, C>(a, grid, stream);
-    return launch_rows<D, 16, T, C>(a, grid, stream);
+    const auto go = [&](void (*row)(ScoreArgs), void (*block)(ScoreArgs)) {
+        return launch(a.window == 1 ? row : block, grid, dim3(kBlock), stream, a);
+    };
+    if (a.heads == 1) return go(score_row_kernel<D, 1, T, C>, score_block_kernel<D, 1, false, T, C>);
+    if (a.heads == 2) return go(score_row_kernel<D, 2, T, C>, score_block_kernel<D, 2, false, T, C>);
+    if (a.heads <= 4) return go(score_row_kernel<D, 4, T, C>, score_block_kernel<D, 4, false, T, C>);
+    if (a.heads <= 8) return go(score_row_kernel<D, 8, T, C>, score_block_kernel<D, 8, false, T, C>);
+    if (a.heads <= 16) return go(score_row_kernel<D, 16, T, C>, score_block_kernel<D, 16, false, T, C>);
+    return go(score_row_kernel<D, 16, T, C>, score_block_kernel<D, 16, true, T, C>);
 }
 
 template <int D>
@@ -338,17 +370,22 @@ extern "C" int paged_kv_score(const paged_kv_cache *cache, int32_t act, const vo
                    lp, q, q_row, q_head, heads, w, table, table_stride, table_width, row_request, row_lengths,
                    n_requests, n_rows, 1, 1, scale, scores, row_offsets};
     const int64_t cap = (int64_t)table_width << lp;
+    dim3 grid;
     int tokens = kBlock / 64 * 32 * tokens_of(cache->head_dim, heads > 2 ? 4 : 1);  // of a workgroup's step
     if (n_rows > n_requests || n_rows > 65535) {
-        // rows share their keys: 128 of them to a workgroup
-        a.window = 128;
-        while (((int64_t)n_rows + a.window - 1) / a.window > 65535) a.window *= 2;
+        // rows share their keys: as many to a workgroup as its LDS holds, and so
+        // many workgroups to a window as give the card 1024 (2 to a CU are resident)
+        const int hp = heads > 8 ? (heads + 15) / 16 * 16 : heads > 4 ? 8 : heads > 2 ? 4 : heads;
+        a.window = window_of(cache->head_dim) / hp;
+        const int64_t windows = ((int64_t)n_rows + a.window - 1) / a.window;
+        const int64_t blocks = (cap + tokens - 1) / tokens, want = (1024 + windows - 1) / windows;
+        grid = dim3((unsigned)windows, (unsigned)(want < blocks ? want : blocks));
     } else {
         // a workgroup's steps: up to 4, as long as 1024 workgroups are left
         while (a.steps < 4 && cap / (2 * a.steps * tokens) * n_rows >= 1024) a.steps *= 2;
         tokens *= a.steps;
+        grid = dim3((unsigned)((cap + tokens - 1) / tokens), (unsigned)n_rows);
     }
-    const dim3 grid((unsigned)((cap + tokens - 1) / tokens), (unsigned)((n_rows + a.window - 1) / a.window));
     return cache->head_dim == 64 ? launch_dim<64>(a, act, cache->code, grid, stream)
                                  : launch_dim<128>(a, act, cache->code, grid, stream);
 }
