@@ -91,54 +91,49 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
             for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
         float m = kLow, l = 0.0f, ref = 0.0f, inv = 0.0f;
 
-        // codes on their way: pages a tile ahead of codes, codes a tile ahead of use
-        int kpage[KN], vpage[VN], spage = -1;
+        // Codes on their way: pages a tile ahead of codes, codes a tile ahead of use.
+        // Nothing that is loaded is used where it is loaded, not even in a
+        // comparison: that would wait for all of it there.
+        int kpage[KN], vpage[VN], spage;
         u32x4 kc[KN];
         u32 vc[VN][4];
         float sc = 0.0f;
-        const auto page_of = [&](int tok) {
-            if (tok >= gr.len) return -1;
-            const int pg = pages[tok >> a.lp];
-            return pg >= 0 && pg < a.n_pages ? pg : -1;
-        };
+        const int last_tok = max(gr.len - 1, 0);
+        const auto page_at = [&](int tok) { return pages[min(tok, last_tok) >> a.lp]; };
+        const auto in_cache = [&](int pg) { return (u32)pg < (u32)a.n_pages; };
         const auto look_up = [&](int u) {
 #pragma unroll
-            for (int e = 0; e < KN; ++e) kpage[e] = page_of(kTile * u + (tid + e * THREADS) / (D / 16));
+            for (int e = 0; e < KN; ++e) kpage[e] = page_at(kTile * u + (tid + e * THREADS) % KI / (D / 16));
 #pragma unroll
-            for (int e = 0; e < VN; ++e) vpage[e] = page_of(kTile * u + (tid + e * THREADS) / (D / 4) * 4);
-            if (tid < 8) spage = page_of(kTile * u + 16 * (tid & 3));
+            for (int e = 0; e < VN; ++e) vpage[e] = page_at(kTile * u + (tid + e * THREADS) % VI / (D / 4) * 4);
+            spage = page_at(kTile * u + 16 * (tid & 3));
         };
+        u32 vthere, sthere;  // of the codes in vc, and of the scale
         const auto fetch = [&](int u) {
 #pragma unroll
             for (int e = 0; e < KN; ++e) {
-                const int i = tid + e * THREADS;
-                if (KI % THREADS != 0 && i >= KI) break;
-                const int tok = kTile * u + i / (D / 16);
-                const uint8_t *p = a.k + max(kpage[e], 0) * a.page_stride +
+                const int i = (tid + e * THREADS) % KI, tok = kTile * u + i / (D / 16);
+                const uint8_t *p = a.k + (in_cache(kpage[e]) ? kpage[e] : 0) * a.page_stride +
                                    ((int64_t)kvh * P + (tok & (P - 1))) * D + i % (D / 16) * 16;
                 kc[e] = *(const u32x4 *)p;
             }
+            vthere = 0;
 #pragma unroll
             for (int e = 0; e < VN; ++e) {
-                const int i = tid + e * THREADS;
-                if (VI % THREADS != 0 && i >= VI) break;
-                const int tok = kTile * u + i / (D / 4) * 4;
-                const uint8_t *p = a.v + max(vpage[e], 0) * a.page_stride +
+                const int i = (tid + e * THREADS) % VI, tok = kTile * u + i / (D / 4) * 4;
+                const bool there = in_cache(vpage[e]);
+                const uint8_t *p = a.v + (there ? vpage[e] : 0) * a.page_stride +
                                    ((int64_t)kvh * P + (tok & (P - 1))) * D + i % (D / 4) * 4;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const u32 x = *(const u32 *)(p + j * D);
-                    // what is not there is 0 whatever its bytes are
-                    vc[e][j] = vpage[e] >= 0 && tok + j < gr.len ? x : 0u;
-                }
+                for (int j = 0; j < 4; ++j) vc[e][j] = *(const u32 *)(p + j * D);
+                // how many of the four tokens are there
+                vthere |= (u32)(there ? min(max(gr.len - tok, 0), 4) : 0) << (4 * e);
             }
-            if (tid < 8) {
-                sc = 0.0f;
-                if (spage >= 0)
-                    sc = tid < 4 ? a.ks[spage * a.scale_stride + kvh] * a.scale2 : a.vs[spage * a.scale_stride + kvh];
-            }
+            const bool there = in_cache(spage) && kTile * u + 16 * (tid & 3) < gr.len;
+            sthere = there;
+            sc = (tid < 4 ? a.ks : a.vs)[(there ? spage : 0) * a.scale_stride + kvh];
         };
-        const auto lay_out = [&](Buffers<D, WAVES> &b, int spage_of) {
+        const auto lay_out = [&](Buffers<D, WAVES> &b) {
 #pragma unroll
             for (int e = 0; e < KN; ++e) {
                 const int i = tid + e * THREADS;
@@ -158,29 +153,30 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
                 const int chunk = (quad >> 2) * 2 + (quad & 1), half = (quad >> 1) & 1;
                 u32 x[4];
                 transpose4(vc[e][0], vc[e][1], vc[e][2], vc[e][3], x);
+                // bytes of tokens that are not there are 0 whatever they hold
+                const u32 n = (vthere >> (4 * e)) & 7, keep = n == 4 ? ~0u : (1u << (8 * n)) - 1;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    *(u32x2 *)&b.v[d + j][16 * swizzled(d + j, chunk) + 8 * half] = Four<C, f16>::of(x[j]);
+                    *(u32x2 *)&b.v[d + j][16 * swizzled(d + j, chunk) + 8 * half] = Four<C, f16>::of(x[j] & keep);
             }
-            if (tid < 4) b.kf[tid] = sc;
-            else if (tid < 8) b.vf[tid - 4] = sc;
-            const u32 there = (u32)__ballot(tid < 4 && spage_of >= 0);
-            if (tid == 0) b.valid = there;
+            const float s = sthere ? sc : 0.0f;
+            if (tid < 4) b.kf[tid] = s * a.scale2;
+            else if (tid < 8) b.vf[tid - 4] = s;
+            const u32 valid = (u32)__ballot(tid < 4 && sthere);
+            if (tid == 0) b.valid = valid;
         };
 
         if (unit < end) {
             look_up(unit);
             fetch(unit);
-            int spage_now = spage;
             if (unit + 1 < end) look_up(unit + 1);
-            lay_out(buf[0], spage_now);
+            lay_out(buf[0]);
             __syncthreads();
             for (int u = unit; u < end; ++u) {
                 const Buffers<D, WAVES> &b = buf[(u - unit) & 1];
                 if (u + 1 < end) {
                     fetch(u + 1);
-                    spage_now = spage;
-                    if (u + 2 < end) look_up(u + 2);
+                    look_up(u + 2);
                 }
                 const int tok0 = kTile * u;
                 if (tok0 < longest) {
@@ -244,7 +240,7 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
                             }
                     }
                 }
-                if (u + 1 < end) lay_out(buf[(u + 1 - unit) & 1], spage_now);
+                if (u + 1 < end) lay_out(buf[(u + 1 - unit) & 1]);
                 __syncthreads();
             }
         }

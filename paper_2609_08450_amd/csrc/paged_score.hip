@@ -59,19 +59,24 @@ struct Rows {
 template <int D, int NT>
 struct Keys {
     u32x4 x[NT][D / 32];
-    float scale;  // times the call's; -inf where the page is not in the cache
+    float raw;   // the page's scale
+    bool there;  // the page is in the cache
+
+    // The page's scale times the call's, or -inf.  (Apart from the load: what uses
+    // a loaded value waits for it, and for the codes loaded before it.)
+    __device__ float scale(float call) const { return there ? raw * call : -__builtin_inff(); }
 };
 
 template <int D, int NT>
 __device__ void load_keys(Keys<D, NT> &k, const ScoreArgs &a, int pg, int tok, int g) {
-    const bool there = pg >= 0 && pg < a.n_pages;
-    const uint8_t *p = a.k + (there ? pg : 0) * a.page_stride + (int64_t)(tok & ((1 << a.lp) - 1)) * D + 16 * g;
+    k.there = pg >= 0 && pg < a.n_pages;
+    const int at = k.there ? pg : 0;
+    const uint8_t *p = a.k + at * a.page_stride + (int64_t)(tok & ((1 << a.lp) - 1)) * D + 16 * g;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) k.x[t][j] = *(const u32x4 *)(p + t * D + 32 * j);
-    k.scale = there ? a.ks[pg * a.scale_stride] : 0.0f;
-    k.scale = there ? k.scale * a.scale : -__builtin_inff();
+    k.raw = a.ks[at * a.scale_stride];
 }
 
 template <int D, class T>
@@ -194,7 +199,7 @@ __global__ __launch_bounds__(kBlock, 2) void score_block_kernel(ScoreArgs a) {
                     k[t][2 * j] = eight<C, T>(raw.x[t][j][0], raw.x[t][j][1]);
                     k[t][2 * j + 1] = eight<C, T>(raw.x[t][j][2], raw.x[t][j][3]);
                 }
-            const float scale = raw.scale;
+            const float scale = raw.scale(a.scale);
             const int next = (int)min((int64_t)base + step, (int64_t)0x7FFFFFFF - STEP);
             if (next < top) {
                 load_keys<D, NT>(raw, a, page, next + NT * n, g);
@@ -322,7 +327,7 @@ __global__ __launch_bounds__(kBlock, D == 64 ? 4 : 2) void score_row_kernel(Scor
                 for (int t = 0; t < NT; ++t) sum[t] = fmaf(w, relu(x[t][i]), sum[t]);
             }
         }
-        if (g == 0) put<NT>(out + tile + NT * n, sum, now.scale, len - (tile + NT * n));
+        if (g == 0) put<NT>(out + tile + NT * n, sum, now.scale(a.scale), len - (tile + NT * n));
         if (more) now = next;
     }
 }
