@@ -12,7 +12,7 @@
  * The cache.  A page holds `page` consecutive tokens of one request; entry
  * [p][h][i][d] of `k` and `v` is an 8-bit code (OCP e4m3 or int8), and
  * k_scale[p][h], v_scale[p][h] are the FP32 scales of a page's entries of one
- * head: value = code * scale.  Token t of request r lies in page
+ * head, not negative: value = code * scale.  Token t of request r lies in page
  * table[r][t / page], at t % page.  Entries past a request's length may hold
  * anything; entries within it are finite (the store writes no others).
  *
@@ -129,7 +129,8 @@ size_t paged_kv_attend_workspace(int32_t n_rows, int32_t n_requests, int32_t hea
  *   out     [n_rows][heads][head_dim], of q's type, contiguous, 16-byte aligned;
  *   lse     FP32 [n_rows][heads], log sum exp of the scaled products, or NULL;
  *   table   int32 [n_requests][table_stride], table_width entries used;
- *   heads   a multiple of the cache's n_heads.
+ *   heads   a multiple of the cache's n_heads;
+ *   scale   finite and not negative.
  * A row that sees no token, or that no request has, gets 0 and -inf. */
 int paged_kv_attend(const paged_kv_cache *cache, int32_t act, const void *q, int64_t q_row,
                     int64_t q_head, int32_t heads, const int32_t *table, int32_t table_stride,

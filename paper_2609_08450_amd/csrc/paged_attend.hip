@@ -171,7 +171,7 @@ int attend(const paged_kv_cache *cache, int act, const void *q, int64_t q_row, i
     if ((act != PAGED_KV_BF16 && act != PAGED_KV_F16) || n_rows < 0 || n_requests < 0 || heads < 1 ||
         heads % cache->n_heads != 0 || table_width < 1 || table_stride < table_width)
         return PAGED_KV_EINVAL;
-    if (selected && K < 1) return PAGED_KV_EINVAL;
+    if ((selected && K < 1) || !(scale >= 0.0f) || scale > 3e38f) return PAGED_KV_EINVAL;
     if (n_rows == 0) return PAGED_KV_OK;
     if (!q || !out || !row_lengths || (n_requests > 0 && !table) || !aligned16(q) || !aligned16(out) || q_row % 8 ||
         q_head % 8)

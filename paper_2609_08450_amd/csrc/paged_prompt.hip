@@ -15,6 +15,8 @@ namespace paged {
 namespace {
 
 constexpr int kTile = 64;
+constexpr float kNoScale = -200.0f;  // log2 of a scale of 0, near enough: below every scale that a value survives
+constexpr float kFaint = -60.0f;     // values this far (powers of 2) below the largest scale are 0 in f16
 
 // Chunk of 16 bytes of V's row d that holds chunk c: reads of 32 rows and writes
 // of every fourth row both spread over the banks.
@@ -24,7 +26,7 @@ template <int D, int WAVES>
 struct Buffers {
     alignas(16) uint8_t k[kTile][2 * D + 16];
     alignas(16) uint8_t v[D][2 * kTile];
-    float kf[4], vf[4];  // of each 16 tokens
+    float kf[4], lv[4];  // of each 16 tokens: the keys' scale, the values' as a power of 2
     u32 valid;           // bit of each 16 tokens: its page is in the cache
 };
 
@@ -89,7 +91,7 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
         f32x16 o[D / 32];
         for (int t = 0; t < D / 32; ++t)
             for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
-        float m = kLow, l = 0.0f, ref = 0.0f, inv = 0.0f;
+        float m = kLow, l = 0.0f, ref = kLow;  // values are held over 2^ref
 
         // Codes on their way: pages a tile ahead of codes, codes a tile ahead of use.
         // Nothing that is loaded is used where it is loaded, not even in a
@@ -161,7 +163,7 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
             }
             const float s = sthere ? sc : 0.0f;
             if (tid < 4) b.kf[tid] = s * a.scale2;
-            else if (tid < 8) b.vf[tid - 4] = s;
+            else if (tid < 8) b.lv[tid - 4] = s > 0.0f ? __log2f(s) : kNoScale;
             const u32 valid = (u32)__ballot(tid < 4 && sthere);
             if (tid == 0) b.valid = valid;
         };
@@ -181,38 +183,67 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
                 const int tok0 = kTile * u;
                 if (tok0 < longest) {
                     const f32x4 kf = *(const f32x4 *)b.kf;
-                    f32x4 vf = *(const f32x4 *)b.vf;
+                    f32x4 lv = *(const f32x4 *)b.lv;
                     const u32 valid = __builtin_amdgcn_readfirstlane(b.valid);
-                    const float vmax = fmaxf(fmaxf(vf[0], vf[1]), fmaxf(vf[2], vf[3]));
+                    const float vmax = fmaxf(fmaxf(lv[0], lv[1]), fmaxf(lv[2], lv[3]));
                     if (__any(vmax > ref)) {
-                        const float to = 4.0f * vmax, by = ref / to;
+                        const float by = exp2_(ref - (vmax + 2.0f));
 #pragma unroll
                         for (int t = 0; t < D / 32; ++t) o[t] *= by;
-                        ref = to;
-                        inv = 1.0f / to;
+                        ref = vmax + 2.0f;
                     }
-                    vf *= inv;
+                    f32x4 back;  // what takes a weight's scale off again, for the sum
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        lv[i] = fmaxf(lv[i] - ref, kFaint);
+                        back[i] = exp2_(-lv[i]);
+                    }
                     const bool all = valid == 15u && tok0 + kTile <= shortest;
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
+                        // All of LDS's pieces are asked for ahead of the products, and V's ahead of
+                        // the softmax: one after the other each would cost LDS's latency.
+                        typename Act<T>::frag kk[D / 16];
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k)
+                            kk[k] = __builtin_bit_cast(typename Act<T>::frag, *(const u32x4 *)&b.k[32 * t + n][32 * k + 16 * g]);
+                        __builtin_amdgcn_sched_barrier(0);
                         f32x16 s;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
-                        for (int k = 0; k < D / 16; ++k) {
-                            const u32x4 x = *(const u32x4 *)&b.k[32 * t + n][32 * k + 16 * g];
-                            s = Act<T>::mfma32(__builtin_bit_cast(typename Act<T>::frag, x), q[k], s);
-                        }
-                        float top = kLow;
+                        for (int k = 0; k < D / 16; ++k) s = Act<T>::mfma32(kk[k], q[k], s);
+                        f16x8 vv[D / 32][2];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            s[i] *= kf[2 * t + (i >> 3)];
-                            if (!all) {
-                                const int tok = tok0 + 32 * t + 8 * (i >> 2) + 4 * g + (i & 3);
-                                if (tok >= len || !((valid >> (2 * t + (i >> 3))) & 1)) s[i] = -__builtin_inff();
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int d = 0; d < D / 32; ++d) {
+                                const int vd = 32 * d + n;
+                                vv[d][h] = __builtin_bit_cast(
+                                    f16x8, *(const u32x4 *)&b.v[vd][16 * swizzled(vd, 4 * t + 2 * h + g)]);
                             }
-                            top = fmaxf(top, s[i]);
-                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                        // A weight with its value's scale is 2^(s kf + lv - m): one multiply-add and
+                        // one exponential; scales are not negative, so the maximum is taken before them.
+                        u32 gone = 0;
+                        if (!all)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const int tok = tok0 + 32 * t + 8 * (i >> 2) + 4 * g + (i & 3);
+                                if (tok >= len || !((valid >> (2 * t + (i >> 3))) & 1)) gone |= 1u << i;
+                            }
+                        const auto highest = [&](auto masked) {
+                            float x[2];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                x[h] = -__builtin_inff();
+#pragma unroll
+                                for (int i = 8 * h; i < 8 * h + 8; ++i)
+                                    x[h] = fmaxf(x[h], decltype(masked)::value && ((gone >> i) & 1) ? -__builtin_inff() : s[i]);
+                            }
+                            return fmaxf(fmaxf(kLow, x[0] * kf[2 * t]), x[1] * kf[2 * t + 1]);
+                        };
+                        float top = all ? highest(std::false_type{}) : highest(std::true_type{});
                         if (__any(top > m + kSlack)) {
                             top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), m);
                             const float by = exp2_(m - top);
@@ -222,22 +253,29 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
                             m = top;
                         }
                         u32x4 p[2];
+                        const auto weigh = [&](auto masked) {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const float f = kf[2 * t + h], c = lv[2 * t + h] - m;
+                                float e[8], sum = 0.0f;
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    e[i] = exp2_(fmaf(s[8 * h + i], f, c));
+                                    if (decltype(masked)::value && ((gone >> (8 * h + i)) & 1)) e[i] = 0.0f;
+                                    sum += e[i];
+                                }
+                                p[h] = u32x4{pack_f16(e[0], e[1]), pack_f16(e[2], e[3]), pack_f16(e[4], e[5]),
+                                             pack_f16(e[6], e[7])};
+                                l = fmaf(sum, back[2 * t + h], l);
+                            }
+                        };
+                        if (all) weigh(std::false_type{});
+                        else weigh(std::true_type{});
 #pragma unroll
                         for (int h = 0; h < 2; ++h)
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float e0 = exp2_(s[8 * h + 2 * i] - m), e1 = exp2_(s[8 * h + 2 * i + 1] - m);
-                                l += e0 + e1;
-                                p[h][i] = pack_f16(e0 * vf[2 * t + h], e1 * vf[2 * t + h]);
-                            }
-#pragma unroll
-                        for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const int vd = 32 * d + n;
-                                const u32x4 x = *(const u32x4 *)&b.v[vd][16 * swizzled(vd, 4 * t + 2 * h + g)];
-                                o[d] = Act<f16>::mfma32(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, p[h]), o[d]);
-                            }
+                            for (int d = 0; d < D / 32; ++d)
+                                o[d] = Act<f16>::mfma32(vv[d][h], __builtin_bit_cast(f16x8, p[h]), o[d]);
                     }
                 }
                 if (u + 1 < end) lay_out(buf[(u + 1 - unit) & 1]);
@@ -252,7 +290,7 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
         const int64_t at = (int64_t)a.group_units[gb0] * vheads + head * ru + (a.group_units[gi] - a.group_units[gb0]);
         const int s0 = share_of(at, total, shares), s1 = share_of(at + units - 1, total, shares), parts = s1 - s0 + 1;
         if (parts == 1) {
-            const float by = l != 0.0f ? ref / l : 0.0f;
+            const float by = l != 0.0f ? exp2_(ref) / l : 0.0f;
             if (out_at >= 0) {
 #pragma unroll
                 for (int d = 0; d < D / 32; ++d)
@@ -273,7 +311,7 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
                     give4(mine + 2 * COLS + col * D + 32 * d + 8 * b + 4 * g,
-                          f32x4{o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]} * ref);
+                          f32x4{o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]} * exp2_(ref));
             if (arrived_last(&a.tickets[s0], parts, &last)) {
                 join_parts<D, COLS, THREADS>(
                     joined, parts, min(gr.rows * per_row, COLS),

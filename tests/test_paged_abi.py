@@ -85,7 +85,8 @@ def test_bad_arguments_are_refused(paged):
     for change in (dict(act=2), dict(act=-1), dict(rows=-1), dict(P=None), dict(P=4100), dict(q_row=250)):
         for name, call in calls(paged, c, **change).items():
             assert call() == EINVAL, (change, name)
-    for change in (dict(heads=0), dict(heads=3), dict(n=-1), dict(width=0), dict(stride=7), dict(ws=None), dict(ws=4104)):
+    for change in (dict(heads=0), dict(heads=3), dict(n=-1), dict(width=0), dict(stride=7), dict(ws=None), dict(ws=4104),
+                   dict(scale=-0.1), dict(scale=float("nan")), dict(scale=float("inf"))):
         for name, call in calls(paged, c, **change).items():
             if name in ("store", "score"):
                 continue
