@@ -95,45 +95,53 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
 
         // Codes on their way: pages a tile ahead of codes, codes a tile ahead of use.
         // Nothing that is loaded is used where it is loaded, not even in a
-        // comparison: that would wait for all of it there.
-        int kpage[KN], vpage[VN], spage;
+        // comparison: that would wait for all of it there.  A wave's tokens of one
+        // load lie in 16 aligned ones, so in one page: pages are scalars, but loaded as
+        // vectors (`zero` is no constant to the compiler), since LDS's pieces could not
+        // be waited for one by one beside a scalar load.
+        int zero = 0;
+        asm("" : "+v"(zero));
+        int kpage[KN], vpage[VN], spage = 0;
         u32x4 kc[KN];
         u32 vc[VN][4];
         float sc = 0.0f;
-        const int last_tok = max(gr.len - 1, 0);
-        const auto page_at = [&](int tok) { return pages[min(tok, last_tok) >> a.lp]; };
+        const int last_tok = max(gr.len - 1, 0), wave_s = __builtin_amdgcn_readfirstlane(wave);
+        const auto page_at = [&](int tok) { return pages[(min(tok, last_tok) >> a.lp) + zero]; };
         const auto in_cache = [&](int pg) { return (u32)pg < (u32)a.n_pages; };
+        const auto k_tok = [&](int e) { return (64 * wave_s + e * THREADS) % KI / (D / 16); };      // first of the wave's
+        const auto v_tok = [&](int e) { return (64 * wave_s + e * THREADS) % VI / (D / 4) * 4; };
         const auto look_up = [&](int u) {
 #pragma unroll
-            for (int e = 0; e < KN; ++e) kpage[e] = page_at(kTile * u + (tid + e * THREADS) % KI / (D / 16));
+            for (int e = 0; e < KN; ++e) kpage[e] = page_at(kTile * u + k_tok(e));
 #pragma unroll
-            for (int e = 0; e < VN; ++e) vpage[e] = page_at(kTile * u + (tid + e * THREADS) % VI / (D / 4) * 4);
-            spage = page_at(kTile * u + 16 * (tid & 3));
+            for (int e = 0; e < VN; ++e) vpage[e] = page_at(kTile * u + v_tok(e));
+            if (wave_s == 0) spage = page_at(kTile * u + 16 * (lane & 3));
         };
-        u32 vthere, sthere;  // of the codes in vc, and of the scale
+        int vleft[VN];  // tokens from the wave's first of vc on that are there
+        bool sthere = false;
         const auto fetch = [&](int u) {
 #pragma unroll
             for (int e = 0; e < KN; ++e) {
-                const int i = (tid + e * THREADS) % KI, tok = kTile * u + i / (D / 16);
-                const uint8_t *p = a.k + (in_cache(kpage[e]) ? kpage[e] : 0) * a.page_stride +
-                                   ((int64_t)kvh * P + (tok & (P - 1))) * D + i % (D / 16) * 16;
-                kc[e] = *(const u32x4 *)p;
+                const int tok = kTile * u + k_tok(e), pg = __builtin_amdgcn_readfirstlane(kpage[e]);
+                const uint8_t *p = a.k + (in_cache(pg) ? pg : 0) * a.page_stride +
+                                   ((int64_t)kvh * P + (tok & (P - 1))) * D;
+                kc[e] = *(const u32x4 *)(p + (u32)(16 * lane));
             }
-            vthere = 0;
 #pragma unroll
             for (int e = 0; e < VN; ++e) {
-                const int i = (tid + e * THREADS) % VI, tok = kTile * u + i / (D / 4) * 4;
-                const bool there = in_cache(vpage[e]);
-                const uint8_t *p = a.v + (there ? vpage[e] : 0) * a.page_stride +
-                                   ((int64_t)kvh * P + (tok & (P - 1))) * D + i % (D / 4) * 4;
+                const int tok = kTile * u + v_tok(e), pg = __builtin_amdgcn_readfirstlane(vpage[e]);
+                const bool there = in_cache(pg);
+                const uint8_t *p = a.v + (there ? pg : 0) * a.page_stride +
+                                   ((int64_t)kvh * P + (tok & (P - 1))) * D;
+                const u32 at = lane / (D / 4) * 4 * D + lane % (D / 4) * 4;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) vc[e][j] = *(const u32 *)(p + j * D);
-                // how many of the four tokens are there
-                vthere |= (u32)(there ? min(max(gr.len - tok, 0), 4) : 0) << (4 * e);
+                for (int j = 0; j < 4; ++j) vc[e][j] = *(const u32 *)(p + (at + j * D));
+                vleft[e] = there ? gr.len - tok : 0;
             }
-            const bool there = in_cache(spage) && kTile * u + 16 * (tid & 3) < gr.len;
-            sthere = there;
-            sc = (tid < 4 ? a.ks : a.vs)[(there ? spage : 0) * a.scale_stride + kvh];
+            if (wave_s == 0) {
+                sthere = in_cache(spage) && kTile * u + 16 * (lane & 3) < gr.len;
+                sc = (lane < 4 ? a.ks : a.vs)[(sthere ? spage : 0) * a.scale_stride + kvh];
+            }
         };
         const auto lay_out = [&](Buffers<D, WAVES> &b) {
 #pragma unroll
@@ -153,19 +161,24 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
                 const int quad = i / (D / 4), d = i % (D / 4) * 4;
                 // tokens 16 s + 8 half + 4 g + j of 32 lie at 16 s + 8 g + 4 half + j
                 const int chunk = (quad >> 2) * 2 + (quad & 1), half = (quad >> 1) & 1;
+                if (vleft[e] < 64 / (D / 4) * 4) {  // bytes of tokens that are not there are 0 whatever they hold
+                    const int n = vleft[e] - lane / (D / 4) * 4;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) vc[e][j] = j < n ? vc[e][j] : 0u;
+                }
                 u32 x[4];
                 transpose4(vc[e][0], vc[e][1], vc[e][2], vc[e][3], x);
-                // bytes of tokens that are not there are 0 whatever they hold
-                const u32 n = (vthere >> (4 * e)) & 7, keep = n == 4 ? ~0u : (1u << (8 * n)) - 1;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    *(u32x2 *)&b.v[d + j][16 * swizzled(d + j, chunk) + 8 * half] = Four<C, f16>::of(x[j] & keep);
+                    *(u32x2 *)&b.v[d + j][16 * swizzled(d + j, chunk) + 8 * half] = Four<C, f16>::of(x[j]);
             }
-            const float s = sthere ? sc : 0.0f;
-            if (tid < 4) b.kf[tid] = s * a.scale2;
-            else if (tid < 8) b.lv[tid - 4] = s > 0.0f ? __log2f(s) : kNoScale;
-            const u32 valid = (u32)__ballot(tid < 4 && sthere);
-            if (tid == 0) b.valid = valid;
+            if (wave_s == 0) {
+                const float s = sthere ? sc : 0.0f;
+                if (lane < 4) b.kf[lane] = s * a.scale2;
+                else if (lane < 8) b.lv[lane - 4] = s > 0.0f ? __log2f(s) : kNoScale;
+                const u32 valid = (u32)__ballot(lane < 4 && sthere);
+                if (lane == 0) b.valid = valid;
+            }
         };
 
         if (unit < end) {
@@ -203,16 +216,21 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
                     for (int t = 0; t < 2; ++t) {
                         // All of LDS's pieces are asked for ahead of the products, and V's ahead of
                         // the softmax: one after the other each would cost LDS's latency.
-                        typename Act<T>::frag kk[D / 16];
-#pragma unroll
-                        for (int k = 0; k < D / 16; ++k)
-                            kk[k] = __builtin_bit_cast(typename Act<T>::frag, *(const u32x4 *)&b.k[32 * t + n][32 * k + 16 * g]);
-                        __builtin_amdgcn_sched_barrier(0);
                         f32x16 s;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+                        constexpr int AHEAD = D / 16 < 8 ? D / 16 : 8;
 #pragma unroll
-                        for (int k = 0; k < D / 16; ++k) s = Act<T>::mfma32(kk[k], q[k], s);
+                        for (int k0 = 0; k0 < D / 16; k0 += AHEAD) {
+                            typename Act<T>::frag kk[AHEAD];
+#pragma unroll
+                            for (int k = 0; k < AHEAD; ++k)
+                                kk[k] = __builtin_bit_cast(typename Act<T>::frag,
+                                                           *(const u32x4 *)&b.k[32 * t + n][32 * (k0 + k) + 16 * g]);
+                            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                            for (int k = 0; k < AHEAD; ++k) s = Act<T>::mfma32(kk[k], q[k0 + k], s);
+                        }
                         f16x8 vv[D / 32][2];
 #pragma unroll
                         for (int h = 0; h < 2; ++h)
