@@ -3,7 +3,8 @@
 //
 // Work is counted in units (a fixed number of tokens of one group of rows and
 // one cache head) and laid out in one line: requests, of a request its cache
-// heads, of a head its groups, of a group its units.  Workgroup w of W takes
+// heads, of a head its groups, of a group its units (for single rows: rows, of a
+// row its heads, of a head its units).  Workgroup w of W takes
 // the units [w T / W, (w + 1) T / W) of T, whatever rows they belong to, so
 // all end together however long the rows are.  A group that lies in several
 // workgroups' shares is joined by the last of them to arrive: each leaves the
@@ -15,6 +16,7 @@
 namespace paged {
 
 constexpr int kMaxShares = 2048;  // workgroups of a launch; one ticket each
+constexpr int kStreamRows = 1024; // rows of a launch of the kernel for single rows
 constexpr float kLow = -1e30f;    // below every score: the maximum of nothing
 constexpr float kSlack = 8.0f;    // a maximum may be passed by this much (powers of 2) before it moves
 
@@ -35,6 +37,7 @@ struct AttendArgs {
     int table_stride, table_width;
     const int *row_starts, *row_lengths;
     int n_rows, n_requests;
+    int row0;         // first row of this launch, in the kernel for single rows
     int heads, per;   // query heads, and those of a cache head
     int parts;        // cuts of those `per` heads, each a "head" of the plan
     float scale2;     // scale * log2(e): scores are powers of 2

@@ -64,7 +64,14 @@ __global__ __launch_bounds__(kPlan) void plan_kernel(AttendArgs a) {
             gr.row0 = bounded(r) + (g - a.group_base[r]) * R;
             gr.rows = min(R, bounded(r + 1) - gr.row0);
             gr.len = 0;
-            for (int i = 0; i < gr.rows; ++i) gr.len = max(gr.len, a.row_lengths[gr.row0 + i]);
+            // eight at a time: one after the other each would cost a trip to memory
+            for (int i = 0; i < gr.rows; i += 8) {
+                int x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = a.row_lengths[gr.row0 + min(i + j, gr.rows - 1)];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) gr.len = max(gr.len, x[j]);
+            }
             gr.len = (int)min((int64_t)gr.len, cap);
             mine = max((gr.len + a.unit - 1) / a.unit, 1);
             a.groups[g] = gr;
@@ -224,10 +231,18 @@ int attend(const paged_kv_cache *cache, int act, const void *q, int64_t q_row, i
         if (grid > 0x7FFFFFFF) return PAGED_KV_EUNSUPPORTED;
         return launch_stream(a, cache->head_dim, act, cache->code, true, s.tiles, (int)grid, stream);
     }
+    if (!s.prompt) {
+        int rc2 = PAGED_KV_OK;
+        for (int r = 0; r < n_rows && rc2 == PAGED_KV_OK; r += kStreamRows) {
+            a.row0 = r;
+            a.n_rows = n_rows - r < kStreamRows ? n_rows - r : kStreamRows;
+            rc2 = launch_stream(a, cache->head_dim, act, cache->code, false, s.tiles, s.shares, stream);
+        }
+        return rc2;
+    }
     const int planned = launch(plan_kernel, dim3(1), dim3(kPlan), stream, a);
     if (planned != PAGED_KV_OK) return planned;
-    return s.prompt ? launch_prompt(a, cache->head_dim, act, cache->code, s.shares, stream)
-                    : launch_stream(a, cache->head_dim, act, cache->code, false, s.tiles, s.shares, stream);
+    return launch_prompt(a, cache->head_dim, act, cache->code, s.shares, stream);
 }
 
 }  // namespace

@@ -20,6 +20,7 @@ namespace {
 
 constexpr int kBlock = 256;
 constexpr int kUnit = 128;     // tokens: 32 to a wave
+constexpr int kSliceRows = kStreamRows;
 constexpr int kList = 1024;    // selected tokens looked up at a time
 
 // 32 tokens' codes of one lane.
@@ -214,38 +215,100 @@ __device__ void load_q(Wave<D, NT, T, C> &w, const AttendArgs &a, int row, int h
     }
 }
 
-// All tokens of single rows: the plan's groups have one row.
+// Where a row's units begin, for up to kSliceRows rows: every workgroup makes the
+// plan for itself (a launch that makes it for all costs more: 6 us on a row of
+// 131071 tokens).
+struct Plan {
+    int units[kSliceRows + 1];    // prefix sum
+    int starts[kSliceRows + 1];   // row_starts, where they fit
+    int waves[kBlock / 64];
+};
+
+__device__ void make_plan(const AttendArgs &a, Plan &plan) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t cap = (int64_t)a.table_width << a.lp;
+    for (int i = tid; i < a.n_rows; i += kBlock) {
+        const int len = (int)min((int64_t)max(a.row_lengths[a.row0 + i], 0), cap);
+        plan.units[i] = max((len + kUnit - 1) / kUnit, 1);
+    }
+    if (a.n_requests <= kSliceRows)
+        for (int i = tid; i <= a.n_requests; i += kBlock) plan.starts[i] = a.row_starts[i];
+    __syncthreads();
+    const int per = (a.n_rows + kBlock - 1) / kBlock, from = min(tid * per, a.n_rows), to = min(from + per, a.n_rows);
+    int mine = 0;
+    for (int i = from; i < to; ++i) mine += plan.units[i];
+    int sum = mine;
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(sum, d);
+        if (lane >= d) sum += y;
+    }
+    if (lane == 63) plan.waves[wave] = sum;
+    __syncthreads();
+    int at = sum - mine;
+    for (int i = 0; i < wave; ++i) at += plan.waves[i];
+    for (int i = from; i < to; ++i) {
+        const int u = plan.units[i];
+        plan.units[i] = at;
+        at += u;
+    }
+    if (tid == kBlock - 1) plan.units[a.n_rows] = at;
+    __syncthreads();
+}
+
+// Largest i in [0, n) with f(i) <= x, f rising, or 0.
+template <class F>
+__device__ int last_not_above(int n, int64_t x, F f) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (f(mid) <= x) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// All tokens of single rows.
 template <int D, int NT, class T, class C>
 __global__ __launch_bounds__(kBlock, D * NT <= 128 ? 2 : 1) void stream_kernel(AttendArgs a) {
+    __shared__ Plan plan;
     __shared__ Shared<D, NT> sh;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
     const int P = 1 << a.lp;
-    const int64_t total = a.total[0], shares = a.total[1];
-
-    // rows that no request has
-    for (int64_t i = max(a.row_starts[a.n_requests], 0) + (int64_t)blockIdx.x; i < a.n_rows; i += gridDim.x) {
-        for (int e = tid; e < a.heads * D / 2; e += kBlock) ((u32 *)a.out)[i * a.heads * D / 2 + e] = 0;
-        if (a.lse)
-            for (int e = tid; e < a.heads; e += kBlock) a.lse[i * a.heads + e] = -__builtin_inff();
-    }
-    if ((int)blockIdx.x >= shares) return;
-
+    make_plan(a, plan);
+    const int vheads = a.kv_heads * a.parts;
+    const int64_t total = (int64_t)plan.units[a.n_rows] * vheads;
+    // a share of fewer than two units is not worth the joining
+    const int64_t shares = min((int64_t)gridDim.x, (total + 1) / 2);
     const int share = blockIdx.x;
+    if (share >= shares) return;
+
     const int64_t begin = share_start(share, total, shares);
     int64_t left = share_start(share + 1, total, shares) - begin;
-    const int4 st = a.starts[share];
-    int gi = st.x, head = st.y, unit = st.z, r = st.w;
-    const int vheads = a.kv_heads * a.parts;
+    int ri = last_not_above(a.n_rows, begin, [&](int i) { return (int64_t)plan.units[i] * vheads; });
+    int head, unit;
+    {
+        const int units = plan.units[ri + 1] - plan.units[ri];
+        const int64_t in = begin - (int64_t)plan.units[ri] * vheads;
+        head = (int)(in / units);
+        unit = (int)(in - (int64_t)head * units);
+    }
     Wave<D, NT, T, C> w;
     while (left > 0) {
-        const Group gr = a.groups[gi];
-        const int units = a.group_units[gi + 1] - a.group_units[gi];
+        const int row = a.row0 + ri;
+        const int units = plan.units[ri + 1] - plan.units[ri];
         const int end = (int)min((int64_t)units, unit + left);
         const int kvh = head / a.parts, part = head - kvh * a.parts;
         const int head0 = kvh * a.per + part * 16 * NT, heads = min(a.per - part * 16 * NT, 16 * NT);
         w.clear();
-        load_q(w, a, gr.row0, head0, heads);
+        load_q(w, a, row, head0, heads);
 
+        struct { int request, len; } gr;
+        {
+            const bool fits = a.n_requests <= kSliceRows;
+            const int *starts = fits ? plan.starts : a.row_starts;
+            gr.request = a.n_requests > 0 ? last_not_above(a.n_requests, row, [&](int i) { return (int64_t)starts[i]; }) : 0;
+            const bool known = a.n_requests > 0 && row >= starts[gr.request] && row < starts[gr.request + 1];
+            gr.len = known ? (int)min((int64_t)max(a.row_lengths[row], 0), (int64_t)a.table_width << a.lp) : 0;
+        }
         const int *pages = a.table + (int64_t)gr.request * a.table_stride;
         const int64_t head_rows = (int64_t)kvh * P * D;
         // tiles of this wave: 32 tokens at kUnit * u + 32 * wave
@@ -315,24 +378,18 @@ __global__ __launch_bounds__(kBlock, D * NT <= 128 ? 2 : 1) void stream_kernel(A
             }
         }
         join_waves(w, sh);
-        // who else has a part of this group
-        const int gb0 = a.group_base[r], gb1 = a.group_base[r + 1];
-        const int64_t ru = a.group_units[gb1] - a.group_units[gb0];
-        const int64_t at = (int64_t)a.group_units[gb0] * vheads + head * ru + (a.group_units[gi] - a.group_units[gb0]);
+        // who else has a part of this row and head
+        const int64_t at = (int64_t)plan.units[ri] * vheads + (int64_t)head * units;
         const int s0 = share_of(at, total, shares), s1 = share_of(at + units - 1, total, shares);
         const int first_slot = 2 * s0 + (at == share_start(s0, total, shares) ? 0 : 1);
         finish<D, 16 * NT, kBlock, T>(
             a, sh.red, sh.tops, sh.sums, sh.joined, heads, s0 == s1, share == s0 ? first_slot : 2 * share, s0,
-            s1 - s0 + 1, first_slot, [&](int c) { return (int64_t)gr.row0 * a.heads + head0 + c; });
+            s1 - s0 + 1, first_slot, [&](int c) { return (int64_t)row * a.heads + head0 + c; });
         left -= end - unit;
         unit = 0;
-        if (left > 0) {
-            ++gi;
-            if (gi == gb1) {
-                if (++head < vheads) gi = gb0;
-                else head = 0;
-            }
-            if (head == 0 && gi == gb1) r = a.groups[gi].request;
+        if (++head == vheads) {
+            head = 0;
+            ++ri;
         }
     }
 }
