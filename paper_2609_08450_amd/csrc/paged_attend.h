@@ -94,64 +94,73 @@ __device__ inline bool arrived_last(int *ticket, int parts, int *flag) {
     return *flag != 0;
 }
 
-// Joins the parts of a group: top and sum of its first `cols` columns, then
-// weight by weight their values.  `part` gives part p's place.  Every thread
-// reads parts of its own, several at once: one after the other each would cost
-// a trip to memory (128 parts on one row of 131071 tokens: 170 us instead of 50).
-template <int COLS, int BLOCK>
+// Joins the parts of a group's first `cols` columns; `part` gives part p's place.
+// A thread holds four values of a column and goes through parts of its own, eight
+// at once with their maximum and sum beside them: one after the other each would
+// cost a trip to memory (one row of 131071 tokens, 64 parts to a head: 182 us, and
+// 78 with the trips made together).
+template <int BLOCK>
 struct Joined {
-    static constexpr int CHUNK = 64;
-    float top[COLS], sum[COLS];
-    float m[BLOCK / COLS][COLS], l[BLOCK / COLS][COLS];
-    float weight[CHUNK][32];  // of a pass's columns
+    f32x4 o[BLOCK];
+    float m[BLOCK], l[BLOCK];
 };
 
 template <int D, int COLS, int BLOCK, class Part, class Out>
-__device__ void join_parts(Joined<COLS, BLOCK> &j, int parts, int cols, Part part, Out out) {
-    constexpr int SPAN = BLOCK / COLS, CHUNK = Joined<COLS, BLOCK>::CHUNK;
-    const int tid = threadIdx.x, c = tid % COLS, k = tid / COLS;
-    float m = kLow, l = 0.0f;
-    if (c < cols)
-#pragma unroll 4
-        for (int p = k; p < parts; p += SPAN) {
-            const f32x2 x = taken(part(p) + 2 * c);
-            const float to = fmaxf(m, x[0]);
-            l = l * exp2_(m - to) + x[1] * exp2_(x[0] - to);
-            m = to;
-        }
-    j.m[k][c] = m;
-    j.l[k][c] = l;
-    __syncthreads();
-    if (tid < COLS) {
-        float to = kLow, all = 0.0f;
-        for (int i = 0; i < SPAN; ++i) to = fmaxf(to, j.m[i][tid]);
-        for (int i = 0; i < SPAN; ++i) all += j.l[i][tid] * exp2_(j.m[i][tid] - to);
-        j.top[tid] = to;
-        j.sum[tid] = all;
-    }
-    __syncthreads();
-    // columns in passes of as many float4s as there are threads
-    constexpr int PER = BLOCK / (D / 4);  // columns of a pass
-    static_assert(PER <= 32, "weights of a pass");
-    const int pc = tid / (D / 4), d = tid % (D / 4) * 4;
+__device__ void join_parts(Joined<BLOCK> &j, int parts, int cols, Part part, Out out) {
+    constexpr int PER = BLOCK / (D / 4), AHEAD = 8;  // columns of a pass
+    const int tid = threadIdx.x, d = tid % (D / 4) * 4;
     for (int c0 = 0; c0 < cols; c0 += PER) {
-        const int col = c0 + pc;
+        // where a pass has fewer columns, its threads share out the parts
+        int width = PER;
+        while (width / 2 >= cols - c0) width /= 2;
+        const int spans = PER / width, col = c0 + tid / (D / 4) % width, span = tid / (D / 4) / width;
         f32x4 o = {0, 0, 0, 0};
-        for (int p0 = 0; p0 < parts; p0 += CHUNK) {
-            const int n = min(CHUNK, parts - p0);
-            __syncthreads();
-            for (int i = tid; i < n * PER; i += BLOCK) {
-                const int p = i / PER, w = i % PER;
-                if (c0 + w < cols) j.weight[p][w] = exp2_(taken(part(p0 + p) + 2 * (c0 + w))[0] - j.top[c0 + w]);
+        float m = kLow, l = 0.0f;
+        if (col < cols)
+            for (int p0 = span; p0 < parts; p0 += AHEAD * spans) {
+                f32x2 ml[AHEAD];
+                f32x4 v[AHEAD];
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    const float *from = part(min(p0 + i * spans, parts - 1));
+                    ml[i] = taken(from + 2 * col);
+                    v[i] = taken4(from + 2 * COLS + col * D + d);
+                }
+                float to = m;
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    if (p0 + i * spans >= parts) ml[i] = f32x2{kLow, 0.0f};
+                    to = fmaxf(to, ml[i][0]);
+                }
+                const float by = exp2_(m - to);
+                o *= by;
+                l *= by;
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    // (a part that saw nothing has no values either)
+                    const float w = ml[i][1] > 0.0f ? exp2_(ml[i][0] - to) : 0.0f;
+                    l += ml[i][1] * w;
+                    o += v[i] * w;
+                }
+                m = to;
             }
+        if (spans > 1) {
+            j.o[tid] = o;
+            j.m[tid] = m;
+            j.l[tid] = l;
             __syncthreads();
-            if (col < cols)
-#pragma unroll 8
-                for (int p = 0; p < n; ++p) o += taken4(part(p0 + p) + 2 * COLS + col * D + d) * j.weight[p][pc];
+            if (span == 0)
+                for (int i = 1; i < spans; ++i) {
+                    const int at = tid + i * width * (D / 4);
+                    const float to = fmaxf(m, j.m[at]), x = exp2_(m - to), y = exp2_(j.m[at] - to);
+                    o = o * x + j.o[at] * y;
+                    l = l * x + j.l[at] * y;
+                    m = to;
+                }
+            __syncthreads();
         }
-        if (col < cols) out(col, d, o, j.top[col], j.sum[col]);
+        if (col < cols && span == 0) out(col, d, o, m, l);
     }
-    __syncthreads();
 }
 
 template <int D, class T>
@@ -165,7 +174,7 @@ __device__ void write_out(const AttendArgs &a, int64_t at, int d, f32x4 o, float
 // A group's first `cols` columns, in LDS: red[col][D + 4] the weighted values, top
 // and sum the softmax's.  `place` gives a column's output row.
 template <int D, int COLS, int BLOCK, class T, class Place>
-__device__ void finish(const AttendArgs &a, float (*red)[D + 4], float *top, float *sum, Joined<COLS, BLOCK> &joined,
+__device__ void finish(const AttendArgs &a, float (*red)[D + 4], float *top, float *sum, Joined<BLOCK> &joined,
                        int cols, bool whole, int slot, int first_share, int parts, int first_slot, Place place) {
     __shared__ int last;
     const int tid = threadIdx.x;

@@ -36,7 +36,7 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
     constexpr int KI = kTile * D / 16, KN = (KI + THREADS - 1) / THREADS;  // 16-byte pieces of K, and of a thread
     constexpr int VI = (kTile / 4) * (D / 4), VN = (VI + THREADS - 1) / THREADS;  // 4 x 4 pieces of V
     __shared__ Buffers<D, WAVES> buf[2];
-    __shared__ Joined<COLS, THREADS> joined;
+    __shared__ Joined<THREADS> joined;
     __shared__ int last;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, g = lane >> 5;
     const int P = 1 << a.lp;

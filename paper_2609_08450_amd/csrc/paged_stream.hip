@@ -148,7 +148,7 @@ struct Shared {
     float red[16 * NT][D + 4];
     float top[4][16 * NT], sum[4][16 * NT];
     float tops[16 * NT], sums[16 * NT];
-    Joined<16 * NT, kBlock> joined;
+    Joined<kBlock> joined;
 };
 
 // The four waves' results into sh.red, sh.tops and sh.sums.
@@ -276,8 +276,11 @@ __global__ __launch_bounds__(kBlock, D * NT <= 128 ? 2 : 1) void stream_kernel(A
     make_plan(a, plan);
     const int vheads = a.kv_heads * a.parts;
     const int64_t total = (int64_t)plan.units[a.n_rows] * vheads;
-    // a share of fewer than two units is not worth the joining
-    const int64_t shares = min((int64_t)gridDim.x, (total + 1) / 2);
+    // Two workgroups to a CU where each gets 32 units; fewer, down to one to a CU,
+    // where the joining of their parts costs more (one row of 131071 tokens on 8
+    // heads: 67 us with 256 shares of 32 units, 76 with 512 of 16); but for small
+    // calls as many as get two units each (a short batch: 15.7 us, and 21.2 with eight).
+    const int64_t shares = min((int64_t)gridDim.x, max((total + 31) / 32, min((total + 1) / 2, (int64_t)gridDim.x / 2)));
     const int share = blockIdx.x;
     if (share >= shares) return;
 
