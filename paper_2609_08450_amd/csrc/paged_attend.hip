@@ -108,8 +108,6 @@ struct Shape {
     int tiles, cols, parts, rows_per_group, unit, shares, splits;
 };
 
-constexpr int kSelectedGrid = 1024;  // of calls that split their rows
-
 Shape shape_of(int n_rows, int n_requests, int heads, int kv_heads, int dim, bool selected, int K, int cus) {
     Shape s = {};
     const int per = heads / kv_heads;
@@ -122,8 +120,9 @@ Shape shape_of(int n_rows, int n_requests, int heads, int kv_heads, int dim, boo
         s.parts = (per + s.cols - 1) / s.cols;
         const int64_t items = (int64_t)n_rows * kv_heads * s.parts;
         const int units = (K + s.unit - 1) / s.unit;
-        // rows are split while that keeps the card's workgroups within kSelectedGrid
-        while (s.splits < units && items * (s.splits + 1) <= kSelectedGrid) ++s.splits;
+        // rows are split while all workgroups are resident at once, two to a CU (the
+        // decode batch: 25.7 us, and 31.0 with two rounds of them)
+        while (s.splits < units && items * (s.splits + 1) <= 2 * cus) ++s.splits;
         s.shares = s.splits > 1 ? (int)(items * s.splits) : 0;
         return s;
     }

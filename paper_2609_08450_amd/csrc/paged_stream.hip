@@ -406,7 +406,11 @@ __global__ __launch_bounds__(kBlock, D * NT <= 128 ? 2 : 1) void selected_kernel
     __shared__ u32 vmax;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, g = lane >> 4;
     const int P = 1 << a.lp, vheads = a.kv_heads * a.parts;
-    const int item = blockIdx.x / a.splits, split = blockIdx.x - item * a.splits;
+    // neighbouring rows on one XCD (workgroups go round them), whose L2 then serves
+    // the tokens that such rows share
+    const int eighth = gridDim.x / 8, b = blockIdx.x;
+    const int w0 = b < 8 * eighth ? (b % 8) * eighth + b / 8 : b;
+    const int item = w0 / a.splits, split = w0 - item * a.splits;
     const int row = item / vheads, head = item - row * vheads;
     const int kvh = head / a.parts, part = head - kvh * a.parts;
     const int head0 = kvh * a.per + part * 16 * NT, heads = min(a.per - part * 16 * NT, 16 * NT);
