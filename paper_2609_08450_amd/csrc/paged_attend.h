@@ -17,6 +17,7 @@ namespace paged {
 
 constexpr int kMaxShares = 2048;  // workgroups of a launch; one ticket each
 constexpr int kStreamRows = 1024; // rows of a launch of the kernel for single rows
+constexpr int kSelectedUnit = 256; // selected tokens that a workgroup takes at a time
 constexpr float kLow = -1e30f;    // below every score: the maximum of nothing
 constexpr float kSlack = 8.0f;    // a maximum may be passed by this much (powers of 2) before it moves
 

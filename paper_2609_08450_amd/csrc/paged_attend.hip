@@ -119,7 +119,7 @@ Shape shape_of(int n_rows, int n_requests, int heads, int kv_heads, int dim, boo
     if (selected) {
         s.parts = (per + s.cols - 1) / s.cols;
         const int64_t items = (int64_t)n_rows * kv_heads * s.parts;
-        const int units = (K + s.unit - 1) / s.unit;
+        const int units = (K + kSelectedUnit - 1) / kSelectedUnit;
         // rows are split while all workgroups are resident at once, two to a CU (the
         // decode batch: 25.7 us, and 31.0 with two rounds of them)
         while (s.splits < units && items * (s.splits + 1) <= 2 * cus) ++s.splits;

@@ -21,7 +21,6 @@ namespace {
 constexpr int kBlock = 256;
 constexpr int kUnit = 128;     // tokens: 32 to a wave
 constexpr int kSliceRows = kStreamRows;
-constexpr int kList = 1024;    // selected tokens looked up at a time
 
 // 32 tokens' codes of one lane.
 template <int D>
@@ -397,14 +396,18 @@ __global__ __launch_bounds__(kBlock, D * NT <= 128 ? 2 : 1) void stream_kernel(A
     }
 }
 
-// The selected tokens of single rows: workgroup = (row, head, split).
+// The selected tokens of single rows: workgroup = (row, head, split).  A wave takes
+// 64 of them at a time, looks them up with a lane to a token, and passes rows and
+// scales to the lanes that read them through LDS of its own.  Each step of a
+// look-up (token, page, scales and codes) is on its way while the 64 before are
+// worked on, and no wave waits for another before the end.
 template <int D, int NT, class T, class C>
 __global__ __launch_bounds__(kBlock, D * NT <= 128 ? 2 : 1) void selected_kernel(AttendArgs a) {
     __shared__ Shared<D, NT> sh;
-    __shared__ u32 rows[kList];  // head row of a token in the cache, or all ones
-    __shared__ float kf[kList], vf[kList];
-    __shared__ u32 vmax;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, g = lane >> 4;
+    // of two times 64 tokens: head row in the cache, or all ones, and the scales
+    __shared__ alignas(16) u32 rows[kBlock / 64][2][64];
+    __shared__ alignas(16) float kf[kBlock / 64][2][64], vf[kBlock / 64][2][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
     const int P = 1 << a.lp, vheads = a.kv_heads * a.parts;
     // neighbouring rows on one XCD (workgroups go round them), whose L2 then serves
     // the tokens that such rows share
@@ -414,89 +417,101 @@ __global__ __launch_bounds__(kBlock, D * NT <= 128 ? 2 : 1) void selected_kernel
     const int row = item / vheads, head = item - row * vheads;
     const int kvh = head / a.parts, part = head - kvh * a.parts;
     const int head0 = kvh * a.per + part * 16 * NT, heads = min(a.per - part * 16 * NT, 16 * NT);
-    const int units = (a.K + kUnit - 1) / kUnit;
-    const int from = (int)((int64_t)units * split / a.splits) * kUnit;
-    const int stop = min((int)((int64_t)units * (split + 1) / a.splits) * kUnit, a.K);
+    const int units = (a.K + kSelectedUnit - 1) / kSelectedUnit;
+    const int from = (int)((int64_t)units * split / a.splits) * kSelectedUnit;
+    const int stop = (int)min((int64_t)units * (split + 1) / a.splits * kSelectedUnit, (int64_t)a.K);
+    const int *list = a.idx + (int64_t)row * a.K;
+    const int first = from + 64 * wave;  // of this wave's tokens, then every kSelectedUnit on
+    const auto token = [&](int q) {
+        const int64_t i = (int64_t)first + (int64_t)q * kSelectedUnit + lane;
+        return i < stop ? list[i] : -1;
+    };
+    int t0 = token(0), t1 = token(1), t2 = token(2);
     const int request = a.row_request[row];
     const bool known = request >= 0 && request < a.n_requests;
-    const int len = known ? min((int64_t)max(a.row_lengths[row], 0), (int64_t)a.table_width << a.lp) : 0;
+    const int len = known ? (int)min((int64_t)max(a.row_lengths[row], 0), (int64_t)a.table_width << a.lp) : 0;
     const int *pages = a.table + (int64_t)(known ? request : 0) * a.table_stride;
-    const int *list = a.idx + (int64_t)row * a.K;
     const u32 page_rows = (u32)(a.page_stride / D);
+    const auto page_of = [&](int t) { return t >= 0 && t < len ? pages[t >> a.lp] : -1; };
+    const auto row_of = [&](int t, int pg) {
+        return (u32)pg < (u32)a.n_pages ? (u32)pg * page_rows + (u32)(kvh * P + (t & (P - 1))) : ~0u;
+    };
 
     Wave<D, NT, T, C> w;
     w.clear();
     load_q(w, a, row, head0, heads);
-    for (int base = from; base < stop; base += kList) {
-        if (tid == 0) vmax = 0;
-        __syncthreads();
-        const int n = min(stop - base, kList), up = (n + kUnit - 1) / kUnit * kUnit;
-        float big = 0.0f;
-        for (int i = tid; i < up; i += kBlock) {
-            u32 at = ~0u;
-            float ks = 0.0f, vs = 0.0f;
-            const int t = i < n ? list[base + i] : -1;
-            if (t >= 0 && t < len) {
-                const int pg = pages[t >> a.lp];
-                if (pg >= 0 && pg < a.n_pages) {
-                    at = (u32)pg * page_rows + (u32)(kvh * P + (t & (P - 1)));
-                    ks = a.ks[pg * a.scale_stride + kvh] * a.scale2;
-                    vs = a.vs[pg * a.scale_stride + kvh];
-                }
-            }
-            rows[i] = at;
-            kf[i] = ks;
-            vf[i] = vs;
-            big = fmaxf(big, vs);
+    const auto load = [&](Tile<D> &x, int at, int i) {
+        const u32 *r = rows[wave][at] + i;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const u32 kr = r[16 * h + m];
+            const uint8_t *kp = a.k + (uint64_t)(kr == ~0u ? 0u : kr) * D;
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j) x.k[h][j] = *(const u32x4 *)(kp + g * 16 + 64 * j);
+            const u32x4 vr = *(const u32x4 *)&r[16 * h + 4 * g];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                load_v<D>(x.v[h][e], a.v + (uint64_t)(vr[e] == ~0u ? 0u : vr[e]) * D + m * (D / 16));
         }
-        for (int d = 32; d; d >>= 1) big = fmaxf(big, __shfl_xor(big, d));
-        if (lane == 0 && big > 0.0f) atomicMax(&vmax, __float_as_uint(big));
-        __syncthreads();
-        w.reference(__uint_as_float(vmax));
-        const auto load = [&](Tile<D> &x, int i) {
+    };
+    const auto take = [&](const Tile<D> &x, int at, int i) {
+        u32 seen = 0;
+        float k2[2][4], v2[2][4];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const u32 kr = rows[i + 16 * h + m];
-                const uint8_t *kp = a.k + (uint64_t)(kr == ~0u ? 0u : kr) * D;
+        for (int h = 0; h < 2; ++h) {
+            const int j = i + 16 * h + 4 * g;
+            const u32x4 r = *(const u32x4 *)&rows[wave][at][j];
+            const f32x4 ks = *(const f32x4 *)&kf[wave][at][j], vs = *(const f32x4 *)&vf[wave][at][j];
 #pragma unroll
-                for (int j = 0; j < D / 64; ++j) x.k[h][j] = *(const u32x4 *)(kp + g * 16 + 64 * j);
-                const u32x4 vr = *(const u32x4 *)&rows[i + 16 * h + 4 * g];
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    load_v<D>(x.v[h][e], a.v + (uint64_t)(vr[e] == ~0u ? 0u : vr[e]) * D + m * (D / 16));
-            }
-        };
-        const auto take = [&](const Tile<D> &x, int i) {
-            u32 seen = 0;
-            float k2[2][4], v2[2][4];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int at = i + 16 * h + 4 * g;
-                const u32x4 r = *(const u32x4 *)&rows[at];
-                const f32x4 ks = *(const f32x4 *)&kf[at], vs = *(const f32x4 *)&vf[at];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    seen |= (r[e] != ~0u ? 1u : 0u) << (4 * h + e);
-                    k2[h][e] = ks[e];
-                    v2[h][e] = vs[e] * w.inv;
-                }
-            }
-            if (__all(seen == 0xFF)) w.take(x, 0xFF, true, k2, v2);
-            else if (__any(seen != 0)) w.take(x, seen, false, k2, v2);
-        };
-        const int last = up;
-        if (32 * wave < last) {
-            Tile<D> x, y;
-            load(x, 32 * wave);
-            for (int i = 32 * wave; i < last; i += 2 * kUnit) {
-                if (i + kUnit < last) load(y, i + kUnit);
-                take(x, i);
-                if (i + kUnit >= last) break;
-                if (i + 2 * kUnit < last) load(x, i + 2 * kUnit);
-                take(y, i + kUnit);
+            for (int e = 0; e < 4; ++e) {
+                seen |= (r[e] != ~0u ? 1u : 0u) << (4 * h + e);
+                k2[h][e] = ks[e];
+                v2[h][e] = vs[e] * w.inv;
             }
         }
-        __syncthreads();
+        if (__all(seen == 0xFF)) w.take(x, 0xFF, true, k2, v2);
+        else if (__any(seen != 0)) w.take(x, seen, false, k2, v2);
+    };
+    const auto put_scales = [&](int at, bool there, float ks, float vs) {
+        kf[wave][at][lane] = there ? ks * a.scale2 : 0.0f;
+        vs = there ? vs : 0.0f;
+        vf[wave][at][lane] = vs;
+        if (__any(vs > w.ref)) {
+            for (int d = 32; d; d >>= 1) vs = fmaxf(vs, __shfl_xor(vs, d));
+            w.reference(vs);
+        }
+        __builtin_amdgcn_wave_barrier();
+    };
+    if (first < stop) {
+        const int times = (stop - first + kSelectedUnit - 1) / kSelectedUnit;
+        Tile<D> x, y;
+        int p1 = page_of(t1);
+        {
+            const int p0 = page_of(t0);
+            const u32 r = row_of(t0, p0);
+            const int64_t s = (int64_t)(r == ~0u ? 0 : p0) * a.scale_stride + kvh;
+            const float ks = a.ks[s], vs = a.vs[s];
+            rows[wave][0][lane] = r;
+            __builtin_amdgcn_wave_barrier();
+            load(x, 0, 0);
+            put_scales(0, r != ~0u, ks, vs);
+        }
+        for (int q = 0; q < times; ++q) {
+            const int at = q & 1;
+            load(y, at, 32);
+            take(x, at, 0);
+            const u32 r = row_of(t1, p1);
+            const int64_t s = (int64_t)(r == ~0u ? 0 : p1) * a.scale_stride + kvh;
+            const float ks = a.ks[s], vs = a.vs[s];
+            rows[wave][at ^ 1][lane] = r;
+            __builtin_amdgcn_wave_barrier();
+            t1 = t2;
+            p1 = page_of(t1);
+            t2 = token(q + 3);
+            if (q + 1 < times) load(x, at ^ 1, 0);
+            take(y, at, 32);
+            put_scales(at ^ 1, r != ~0u, ks, vs);
+        }
     }
     join_waves(w, sh);
     // splits of an item have neighbouring workgroups: shares item * splits + split
