@@ -97,6 +97,13 @@ def _ptr(t, dtype, shape, name):
     return t.data_ptr()
 
 
+def _vec(t, dtype, n, name):
+    """_ptr of a tensor with one axis, in fewer steps: the short calls' host time counts."""
+    if t.dtype is dtype and t.is_cuda and t.numel() == n and t.dim() == 1 and t.is_contiguous():
+        return t.data_ptr()
+    return _ptr(t, dtype, (n,), name)
+
+
 def _rows3(t, heads, dim, name):
     """Address and strides of activations [rows, heads, dim] whose last axis is contiguous."""
     if not t.is_cuda:
@@ -226,11 +233,11 @@ def tables(ring, pool, lens, new_lens, table, page: int, *, pool_out, lens_out, 
     i32 = torch.int32
     at, stride, width = _table(table, n)
     _check((_lib or lib()).paged_kv_tables(
-        _ptr(ring, i32, (None,), "ring"), ring.numel(), _ptr(pool, i32, (4,), "pool"),
-        _ptr(pool_out, i32, (4,), "pool_out"), _ptr(lens, i32, (n,), "lens"), _ptr(new_lens, i32, (n,), "new_lens"),
-        _ptr(lens_out, i32, (n,), "lens_out"), n, at, stride, width, page, rows,
-        _ptr(row_starts, i32, (n + 1,), "row_starts"), _ptr(row_request, i32, (rows,), "row_request"),
-        _ptr(row_lengths, i32, (rows,), "row_lengths"), _ptr(slots, torch.int64, (rows,), "slots"),
+        _ptr(ring, i32, (None,), "ring"), ring.numel(), _vec(pool, i32, 4, "pool"),
+        _vec(pool_out, i32, 4, "pool_out"), _vec(lens, i32, n, "lens"), _vec(new_lens, i32, n, "new_lens"),
+        _vec(lens_out, i32, n, "lens_out"), n, at, stride, width, page, rows,
+        _vec(row_starts, i32, n + 1, "row_starts"), _vec(row_request, i32, rows, "row_request"),
+        _vec(row_lengths, i32, rows, "row_lengths"), _vec(slots, torch.int64, rows, "slots"),
         _topk._stream(stream)), "paged_kv_tables")
 
 
@@ -246,7 +253,7 @@ def store(cache: PagedCache, k_new, v_new, slots, stream=None) -> None:
     if (v_new is None) != (cache.v is None):
         raise PagedError("v_new belongs to a cache with values, and to no other")
     _check((_lib or lib()).paged_kv_store(cache._ref, ACTS[k_new.dtype], k, k_row, k_head, v, v_row, v_head,
-                                          _ptr(slots, torch.int64, (n,), "slots"), n, _topk._stream(stream)),
+                                          _vec(slots, torch.int64, n, "slots"), n, _topk._stream(stream)),
            "paged_kv_store")
 
 
@@ -269,8 +276,8 @@ def attend(cache: PagedCache, q, table, row_starts, row_lengths, scale: float, o
     ws, size = cache._space(workspace, rows, n, heads)
     _check((_lib or lib()).paged_kv_attend(
         cache._ref, ACTS[q.dtype], qp, q_row, q_head, heads, at, stride, width,
-        _ptr(row_starts, torch.int32, (n + 1,), "row_starts"), n,
-        _ptr(row_lengths, torch.int32, (rows,), "row_lengths"), rows, scale, op, lp, ws, size,
+        _vec(row_starts, torch.int32, n + 1, "row_starts"), n,
+        _vec(row_lengths, torch.int32, rows, "row_lengths"), rows, scale, op, lp, ws, size,
         _topk._stream(stream)), "paged_kv_attend")
     return out
 
@@ -287,8 +294,8 @@ def attend_selected(cache: PagedCache, q, idx, table, row_request, row_lengths, 
     ws, size = cache._space(workspace, rows, n, heads)
     _check((_lib or lib()).paged_kv_attend_selected(
         cache._ref, ACTS[q.dtype], qp, q_row, q_head, heads, _ptr(idx, torch.int32, (rows, None), "idx"),
-        idx.shape[1], at, stride, width, _ptr(row_request, torch.int32, (rows,), "row_request"), n,
-        _ptr(row_lengths, torch.int32, (rows,), "row_lengths"), rows, scale, op, lp, ws, size,
+        idx.shape[1], at, stride, width, _vec(row_request, torch.int32, rows, "row_request"), n,
+        _vec(row_lengths, torch.int32, rows, "row_lengths"), rows, scale, op, lp, ws, size,
         _topk._stream(stream)), "paged_kv_attend_selected")
     return out
 
@@ -302,7 +309,7 @@ def score(cache: PagedCache, q, w, table, row_request, row_lengths, scale: float
     at, stride, width = _table(table)
     _check((_lib or lib()).paged_kv_score(
         cache._ref, ACTS[q.dtype], qp, q_row, q_head, heads, _ptr(w, torch.float32, (rows, heads), "w"), at, stride,
-        width, _ptr(row_request, torch.int32, (rows,), "row_request"), table.shape[0],
-        _ptr(row_lengths, torch.int32, (rows,), "row_lengths"), rows, scale,
-        _ptr(scores, torch.float32, scores.shape, "scores"), _ptr(row_offsets, torch.int64, (rows,), "row_offsets"),
+        width, _vec(row_request, torch.int32, rows, "row_request"), table.shape[0],
+        _vec(row_lengths, torch.int32, rows, "row_lengths"), rows, scale,
+        _ptr(scores, torch.float32, scores.shape, "scores"), _vec(row_offsets, torch.int64, rows, "row_offsets"),
         _topk._stream(stream)), "paged_kv_score")
