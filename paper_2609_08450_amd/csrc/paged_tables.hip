@@ -134,11 +134,22 @@ __global__ __launch_bounds__(BLOCK) void tables_kernel(TablesArgs a, bool own) {
         // four pages of a thread at once: one after the other each would cost its trips to memory
         for (int i0 = tid; i0 < count; i0 += 4 * BLOCK) {
             int32_t *entry[4], *place[4], page[4];
+            int i[4], k[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int i = min(i0 + j * BLOCK, count - 1), k = last_start(order, n, i);
-                entry[j] = a.table + (int64_t)(base + k) * a.stride + column[k] + (i - order[k]);
-                place[j] = a.ring + (first + (u32)i) % (u32)size;
+                i[j] = min(i0 + j * BLOCK, count - 1);
+                k[j] = 0;
+            }
+            for (int step = BLOCK / 2; step; step >>= 1)  // the last request that starts at or before page i
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int to = k[j] + step;
+                    if (to < n && order[min(to, n - 1)] <= i[j]) k[j] = to;
+                }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                entry[j] = a.table + (int64_t)(base + k[j]) * a.stride + column[k[j]] + (i[j] - order[k[j]]);
+                place[j] = a.ring + (first + (u32)i[j]) % (u32)size;
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) page[j] = to_ring ? *entry[j] : *place[j];
