@@ -16,7 +16,7 @@ namespace {
 
 constexpr int kTile = 64;
 constexpr float kNoScale = -200.0f;  // log2 of a scale of 0, near enough: below every scale that a value survives
-constexpr float kFaint = -60.0f;     // values this far (powers of 2) below the largest scale are 0 in f16
+constexpr float kFaint = -60.0f;     // values this far (powers of 2) below the reference are 0 in f16 weights
 
 // Chunk of 16 bytes of V's row d that holds chunk c: reads of 32 rows and writes
 // of every fourth row both spread over the banks.
@@ -199,11 +199,11 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
                     f32x4 lv = *(const f32x4 *)b.lv;
                     const u32 valid = __builtin_amdgcn_readfirstlane(b.valid);
                     const float vmax = fmaxf(fmaxf(lv[0], lv[1]), fmaxf(lv[2], lv[3]));
-                    if (__any(vmax > ref)) {
-                        const float by = exp2_(ref - (vmax + 2.0f));
+                    if (__any(vmax > ref + 7.0f)) {  // weights stay below 2^(8 + 7) in f16
+                        const float by = exp2_(ref - (vmax - 6.0f));
 #pragma unroll
                         for (int t = 0; t < D / 32; ++t) o[t] *= by;
-                        ref = vmax + 2.0f;
+                        ref = vmax - 6.0f;
                     }
                     f32x4 back;  // what takes a weight's scale off again, for the sum
 #pragma unroll

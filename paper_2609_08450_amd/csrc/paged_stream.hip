@@ -11,8 +11,8 @@
 // bytes are brought to it by 4 x 4 byte transposes.  No value crosses lanes
 // but the maximum, and that only when it moves by more than 2^8.
 // P is rounded to f16 (11 bits, whatever q's type: V's codes are exact in it),
-// weighted with V's scale over the largest one seen so far, so that its range
-// does not depend on the scales.
+// weighted with V's scale over a reference that follows the largest one seen so
+// far, so that its range does not depend on the scales.
 #include "paged_attend.h"
 
 namespace paged {
@@ -60,9 +60,12 @@ struct Wave {
         inv = 0.0f;
     }
 
-    __device__ void reference(float vs) {  // wave-uniform
-        if (vs > ref) {
-            const float to = 4.0f * vs, by = ref / to;
+    // Before tokens whose largest scale is vs (the same in all lanes): f16 weights are
+    // then at most 2^8 (a maximum's slack) * 2^7, and exact to 11 bits down to 2^-20.
+    __device__ bool beyond(float vs) const { return vs > 128.0f * ref; }
+    __device__ void reference(float vs) {
+        if (beyond(vs)) {
+            const float to = vs * 0.015625f, by = ref / to;
             for (int t = 0; t < NT; ++t)
                 for (int j = 0; j < D / 16; ++j) o[t][j] *= by;
             ref = to;
@@ -476,7 +479,7 @@ __global__ __launch_bounds__(kBlock, D * NT <= 128 ? 2 : 1) void selected_kernel
         kf[wave][at][lane] = there ? ks * a.scale2 : 0.0f;
         vs = there ? vs : 0.0f;
         vf[wave][at][lane] = vs;
-        if (__any(vs > w.ref)) {
+        if (__any(w.beyond(vs))) {
             for (int d = 32; d; d >>= 1) vs = fmaxf(vs, __shfl_xor(vs, d));
             w.reference(vs);
         }
