@@ -111,7 +111,7 @@ struct Shape {
 Shape shape_of(int n_rows, int n_requests, int heads, int kv_heads, int dim, bool selected, int K, int cus) {
     Shape s = {};
     const int per = heads / kv_heads;
-    s.tiles = per > 16 ? 2 : 1;
+    s.tiles = per > 16 && dim < 256 ? 2 : 1;
     s.cols = 16 * s.tiles;
     s.rows_per_group = 1;
     s.unit = 128;

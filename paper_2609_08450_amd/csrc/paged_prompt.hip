@@ -231,15 +231,18 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
 #pragma unroll
                             for (int k = 0; k < AHEAD; ++k) s = Act<T>::mfma32(kk[k], q[k0 + k], s);
                         }
-                        f16x8 vv[D / 32][2];
+                        // (half of V's where a head of 256 leaves no registers for more)
+                        constexpr int EARLY = D == 256 ? 1 : 2;
+                        f16x8 vv[EARLY][D / 32];
+                        const auto v_piece = [&](int h, int d) {
+                            const int vd = 32 * d + n;
+                            return __builtin_bit_cast(f16x8,
+                                                      *(const u32x4 *)&b.v[vd][16 * swizzled(vd, 4 * t + 2 * h + g)]);
+                        };
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
+                        for (int h = 0; h < EARLY; ++h)
 #pragma unroll
-                            for (int d = 0; d < D / 32; ++d) {
-                                const int vd = 32 * d + n;
-                                vv[d][h] = __builtin_bit_cast(
-                                    f16x8, *(const u32x4 *)&b.v[vd][16 * swizzled(vd, 4 * t + 2 * h + g)]);
-                            }
+                            for (int d = 0; d < D / 32; ++d) vv[h][d] = v_piece(h, d);
                         __builtin_amdgcn_sched_barrier(0);
                         // A weight with its value's scale is 2^(s kf + lv - m): one multiply-add and
                         // one exponential; scales are not negative, so the maximum is taken before them.
@@ -293,7 +296,8 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
                         for (int h = 0; h < 2; ++h)
 #pragma unroll
                             for (int d = 0; d < D / 32; ++d)
-                                o[d] = Act<f16>::mfma32(vv[d][h], __builtin_bit_cast(f16x8, p[h]), o[d]);
+                                o[d] = Act<f16>::mfma32(h < EARLY ? vv[h % EARLY][d] : v_piece(h, d),
+                                                        __builtin_bit_cast(f16x8, p[h]), o[d]);
                     }
                 }
                 if (u + 1 < end) lay_out(buf[(u + 1 - unit) & 1]);

@@ -526,11 +526,12 @@ __global__ __launch_bounds__(kBlock, D * NT <= 128 ? 2 : 1) void selected_kernel
 template <int D, class T, class C>
 int launch_of(const AttendArgs &a, bool selected, int tiles, int grid, void *stream) {
     const dim3 g((unsigned)grid), b(kBlock);
-    if (selected)
-        return tiles == 1 ? launch(selected_kernel<D, 1, T, C>, g, b, stream, a)
-                          : launch(selected_kernel<D, 2, T, C>, g, b, stream, a);
-    return tiles == 1 ? launch(stream_kernel<D, 1, T, C>, g, b, stream, a)
-                      : launch(stream_kernel<D, 2, T, C>, g, b, stream, a);
+    if constexpr (D < 256)  // (heads of 256 leave no registers for two)
+        if (tiles == 2)
+            return selected ? launch(selected_kernel<D, 2, T, C>, g, b, stream, a)
+                            : launch(stream_kernel<D, 2, T, C>, g, b, stream, a);
+    return selected ? launch(selected_kernel<D, 1, T, C>, g, b, stream, a)
+                    : launch(stream_kernel<D, 1, T, C>, g, b, stream, a);
 }
 
 template <int D>
