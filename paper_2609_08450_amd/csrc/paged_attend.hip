@@ -126,7 +126,10 @@ Shape shape_of(int n_rows, int n_requests, int heads, int kv_heads, int dim, boo
         s.shares = s.splits > 1 ? (int)(items * s.splits) : 0;
         return s;
     }
-    s.prompt = n_rows > n_requests;
+    // up to three rows to a request each row reads the cache by itself (64 rows of 32
+    // requests at 16384 to 32768 tokens: 127 us, and 227 as a
+    // prompt; three to a request: 180 and 230)
+    s.prompt = n_rows > 3 * (int64_t)n_requests;
     if (s.prompt) {
         s.cols = dim == 256 ? 128 : 256;
         s.unit = 64;
