@@ -98,8 +98,8 @@ __device__ inline bool arrived_last(int *ticket, int parts, int *flag) {
 // Joins the parts of a group's first `cols` columns; `part` gives part p's place.
 // A thread holds four values of a column and goes through parts of its own, eight
 // at once with their maximum and sum beside them: one after the other each would
-// cost a trip to memory (one row of 131071 tokens, 64 parts to a head: 182 us, and
-// 78 with the trips made together).
+// cost a trip to memory (one row of 131071 tokens, 32 parts to a head: 57 us, and
+// 67 with maxima and values in passes of their own).
 template <int BLOCK>
 struct Joined {
     f32x4 o[BLOCK];

@@ -188,11 +188,18 @@ int attend(const paged_kv_cache *cache, int act, const void *q, int64_t q_row, i
     if (selected ? !idx || !row_request : !row_starts) return PAGED_KV_EINVAL;
     if (!workspace || ((uintptr_t)workspace & 255) != 0) return PAGED_KV_EINVAL;
     if (!fits(n_rows, n_requests, heads, cache->n_heads, cache->head_dim) ||
-        ((int64_t)table_width << log2_page(cache->page)) > 0x7FFFFFFF - 256)
+        K > 0x7FFFFF00)
         return PAGED_KV_EUNSUPPORTED;
+    // tokens, a few tiles past the last, are 32-bit numbers
+    const int64_t cap = (int64_t)table_width << log2_page(cache->page);
+    if (cap > 0x7FFFFFFF - 8192) return PAGED_KV_EUNSUPPORTED;
     const int cus = device_cus();
     if (cus == 0) return PAGED_KV_EUNSUPPORTED;
     const Shape s = shape_of(n_rows, n_requests, heads, cache->n_heads, cache->head_dim, selected, K, cus);
+    // and so are a plan's units
+    const int64_t groups = s.prompt ? n_rows / s.rows_per_group + (int64_t)n_requests
+                                    : n_rows < kStreamRows ? n_rows : kStreamRows;
+    if (!selected && (double)groups * (double)(cap / s.unit + 1) > 2e9) return PAGED_KV_EUNSUPPORTED;
     AttendArgs a = {};
     if (lay_out(&a, (char *)workspace, s, n_rows, n_requests, cache->head_dim) > bytes) return PAGED_KV_EWORKSPACE;
     a.k = (const uint8_t *)cache->k;

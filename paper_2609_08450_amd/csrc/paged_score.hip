@@ -10,7 +10,7 @@
 //     vector operations behind each of their results (a maximum and a
 //     multiply-add), and by the 4 bytes written for each;
 //   single rows (score_row_kernel): bound by the keys' D bytes a token; every
-//     wave streams tokens of its own, its next codes already on their way.
+//     wave streams tokens of its own.
 #include "paged_common.h"
 
 namespace paged {
@@ -21,7 +21,9 @@ constexpr int kBlock = 256;
 // Tokens of a lane: what the registers hold beside the sums.
 constexpr int tokens_of(int dim, int hp) { return dim == 64 && hp >= 4 ? 4 : 2; }
 
-// In the kernel of single rows: 4 waves to a SIMD beat 2 with twice the tokens (67.4 against 74.7 us on the decode batch).
+// In the kernel of single rows: few tokens to a lane and many waves.  (The decode
+// batch: 68.7 us with 5 waves to a SIMD and 2 tokens to a lane; 73.6 with 4 waves
+// that hold their next codes too; 74.7 with 2 waves of twice the tokens.)
 constexpr int kRowTokens = 2;
 
 struct ScoreArgs {
@@ -257,7 +259,7 @@ __global__ __launch_bounds__(kBlock, 2) void score_block_kernel(ScoreArgs a) {
 
 // Single rows: workgroup = (row, 4 waves x `steps` x 32 NT tokens).
 template <int D, int HP, class T, class C>
-__global__ __launch_bounds__(kBlock, D == 64 ? 4 : 2) void score_row_kernel(ScoreArgs a) {
+__global__ __launch_bounds__(kBlock, D == 64 ? 5 : 3) void score_row_kernel(ScoreArgs a) {
     constexpr int NT = kRowTokens;
     __shared__ alignas(16) uint8_t qs[128][2 * D + 16];
     __shared__ alignas(16) float ws[128];
@@ -287,20 +289,15 @@ __global__ __launch_bounds__(kBlock, D == 64 ? 4 : 2) void score_row_kernel(Scor
     for (int h = tid; h < chunks * HP; h += kBlock) ws[h] = h < a.heads ? a.w[(int64_t)row * a.heads + h] : 0.0f;
     __syncthreads();
 
-    Keys<D, NT> now, next;
-    load_keys<D, NT>(now, a, page, tok0 + NT * n, g);
-    page = page_of(1);
     float *out = a.scores + a.row_offsets[row];
-    // half wave g's places i hold heads of this row where g = 0 alone: the other half repeats them
+    // half wave 0's places i hold the row's heads, and half wave 1 repeats them
     const int mm = ((n >> 3) << 2) + (n & 3);  // place of product row n
     for (int s = 0; s < a.steps; ++s) {
         const int tile = tok0 + s * (kBlock / 64 * 32 * NT);
         if (tile >= len) break;
-        const bool more = s + 1 < a.steps && tile + kBlock / 64 * 32 * NT < len;
-        if (more) {
-            load_keys<D, NT>(next, a, page, tile + kBlock / 64 * 32 * NT + NT * n, g);
-            page = page_of(s + 2);
-        }
+        Keys<D, NT> now;
+        load_keys<D, NT>(now, a, page, tile + NT * n, g);
+        page = page_of(s + 1);
         float sum[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) sum[t] = 0.0f;
@@ -328,7 +325,6 @@ __global__ __launch_bounds__(kBlock, D == 64 ? 4 : 2) void score_row_kernel(Scor
             }
         }
         if (g == 0) put<NT>(out + tile + NT * n, sum, now.scale(a.scale), len - (tile + NT * n));
-        if (more) now = next;
     }
 }
 

@@ -97,6 +97,9 @@ def test_bad_arguments_are_refused(paged):
     assert calls(paged, one, heads=129)["score"]() == EUNSUPPORTED
     assert calls(paged, c)["score"]() == EUNSUPPORTED                   # a cache of two heads
     assert calls(paged, c, K=0)["selected"]() == EINVAL
+    assert calls(paged, c, K=2 ** 31 - 1)["selected"]() == EUNSUPPORTED
+    far = calls(paged, c, width=2 ** 27, stride=2 ** 27)                # more tokens than 32 bits count
+    assert far["attend"]() == EUNSUPPORTED and far["selected"]() == EUNSUPPORTED
     assert calls(paged, one)["attend"]() == EINVAL                      # no values
     assert calls(paged, one)["store"]() == EINVAL                       # v_new without values
     # nothing to do is no error, whatever the pointers
