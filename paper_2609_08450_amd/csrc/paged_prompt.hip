@@ -50,7 +50,11 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
     }
     if ((int)blockIdx.x >= shares) return;
 
-    const int share = blockIdx.x;
+    // neighbouring shares, which read the same keys and values, on one XCD (workgroups
+    // go round them), where every workgroup has one (501 us instead of 510 for 4096 rows
+    // of three prompts)
+    const int eighth = gridDim.x / 8, b8 = blockIdx.x;
+    const int share = shares == gridDim.x && b8 < 8 * eighth ? (b8 % 8) * eighth + b8 / 8 : b8;
     const int64_t begin = share_start(share, total, shares);
     int64_t left = share_start(share + 1, total, shares) - begin;
     const int4 st = a.starts[share];

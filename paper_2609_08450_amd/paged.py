@@ -206,18 +206,21 @@ class PagedCache:
             self._sizes[key] = size
         return size
 
-    def alloc_workspace(self, n_rows: int, n_requests: int, heads: int) -> torch.Tensor:
-        """A workspace for attention calls of up to these sizes, ready for its first use."""
-        ws = torch.empty(self.workspace_size(n_rows, n_requests, heads), dtype=torch.uint8,
-                         device=self.k.device)
-        ws[:WORKSPACE_ZEROED].zero_()
+    def alloc_workspace(self, n_rows: int, n_requests: int, heads: int, stream=None) -> torch.Tensor:
+        """A workspace for attention calls of these sizes, ready for its first use on `stream`."""
+        if stream is not None and not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(_topk._stream(stream))
+        with torch.cuda.stream(stream):
+            ws = torch.empty(self.workspace_size(n_rows, n_requests, heads), dtype=torch.uint8,
+                             device=self.k.device)
+            ws[:WORKSPACE_ZEROED].zero_()
         return ws
 
-    def _space(self, workspace, n_rows, n_requests, heads):
+    def _space(self, workspace, n_rows, n_requests, heads, stream):
         need = self.workspace_size(n_rows, n_requests, heads)
         if workspace is None:
             if self.workspace is None or self.workspace.numel() < need:
-                self.workspace = self.alloc_workspace(n_rows, n_requests, heads)
+                self.workspace = self.alloc_workspace(n_rows, n_requests, heads, stream)
             workspace = self.workspace
         elif workspace.dtype is not torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
             raise PagedError("workspace must be a contiguous device tensor of uint8")
@@ -273,7 +276,7 @@ def attend(cache: PagedCache, q, table, row_starts, row_lengths, scale: float, o
     at, stride, width = _table(table)
     n = table.shape[0]
     out, op, lp = _outputs(cache, q, out, lse)
-    ws, size = cache._space(workspace, rows, n, heads)
+    ws, size = cache._space(workspace, rows, n, heads, stream)
     _check((_lib or lib()).paged_kv_attend(
         cache._ref, ACTS[q.dtype], qp, q_row, q_head, heads, at, stride, width,
         _vec(row_starts, torch.int32, n + 1, "row_starts"), n,
@@ -291,7 +294,7 @@ def attend_selected(cache: PagedCache, q, idx, table, row_request, row_lengths, 
     at, stride, width = _table(table)
     n = table.shape[0]
     out, op, lp = _outputs(cache, q, out, lse)
-    ws, size = cache._space(workspace, rows, n, heads)
+    ws, size = cache._space(workspace, rows, n, heads, stream)
     _check((_lib or lib()).paged_kv_attend_selected(
         cache._ref, ACTS[q.dtype], qp, q_row, q_head, heads, _ptr(idx, torch.int32, (rows, None), "idx"),
         idx.shape[1], at, stride, width, _vec(row_request, torch.int32, rows, "row_request"), n,

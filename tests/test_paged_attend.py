@@ -302,6 +302,24 @@ def test_two_streams():
         assert_attention(out, lse, refs[i % 2], "streams")
 
 
+def test_first_call_on_a_stream_of_its_own():
+    """The cache's own workspace is made ready on the stream that uses it."""
+    from paper_2609_08450_amd import paged
+
+    s = Setup([9000], [1], page=32, kv=1, heads=8, dim=128).cuda()
+    ref, other = attention(s), torch.cuda.Stream()
+    filler = torch.ones(1 << 26, device="cuda")
+    torch.cuda.synchronize()
+    for handle in (other, other.cuda_stream):
+        for _ in range(4):
+            filler.mul_(1.0)  # the current stream is busy meanwhile
+        out, lse = torch.empty_like(s.q), torch.empty((1, 8), device="cuda")
+        other.wait_stream(torch.cuda.current_stream())
+        paged.attend(s.cache(), s.q, s.table, s.row_starts, s.row_lengths, s.scale, out=out, lse=lse, stream=handle)
+        torch.cuda.synchronize()
+        assert_attention(out, lse, ref, "own stream")
+
+
 @pytest.mark.parametrize("prompt", [False, True])
 def test_graph(prompt):
     """Captured once, replayed with eager calls between, each replay on other inputs."""
