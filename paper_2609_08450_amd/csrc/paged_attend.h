@@ -7,8 +7,9 @@
 // row its heads, of a head its units).  Workgroup w of W takes
 // the units [w T / W, (w + 1) T / W) of T, whatever rows they belong to, so
 // all end together however long the rows are.  A group that lies in several
-// workgroups' shares is joined by the last of them to arrive: each leaves the
-// maximum, the sum and the weighted values of its part, in FP32.
+// workgroups' shares is joined from its parts, each with a maximum, a sum and the
+// weighted values in FP32: for single rows by the last workgroup to arrive, for
+// prompts, whose parts are 16 times as large, by a launch of its own.
 #pragma once
 
 #include "paged_common.h"
@@ -95,7 +96,7 @@ __device__ inline bool arrived_last(int *ticket, int parts, int *flag) {
     return *flag != 0;
 }
 
-// Joins the parts of a group's first `cols` columns; `part` gives part p's place.
+// Joins the parts of a group's columns [first, cols); `part` gives part p's place.
 // A thread holds four values of a column and goes through parts of its own, eight
 // at once with their maximum and sum beside them: one after the other each would
 // cost a trip to memory (one row of 131071 tokens, 32 parts to a head: 57 us, and
@@ -107,10 +108,10 @@ struct Joined {
 };
 
 template <int D, int COLS, int BLOCK, class Part, class Out>
-__device__ void join_parts(Joined<BLOCK> &j, int parts, int cols, Part part, Out out) {
+__device__ void join_parts(Joined<BLOCK> &j, int parts, int first, int cols, Part part, Out out) {
     constexpr int PER = BLOCK / (D / 4), AHEAD = 8;  // columns of a pass
     const int tid = threadIdx.x, d = tid % (D / 4) * 4;
-    for (int c0 = 0; c0 < cols; c0 += PER) {
+    for (int c0 = first; c0 < cols; c0 += PER) {
         // where a pass has fewer columns, its threads share out the parts
         int width = PER;
         while (width / 2 >= cols - c0) width /= 2;
@@ -198,7 +199,7 @@ __device__ void finish(const AttendArgs &a, float (*red)[D + 4], float *top, flo
     if (!arrived_last(&a.tickets[first_share], parts, &last)) return;
     // part p lies in slot 0 of share first_share + p, the first one in first_slot
     join_parts<D, COLS, BLOCK>(
-        joined, parts, cols,
+        joined, parts, 0, cols,
         [&](int p) { return a.left + (int64_t)(p == 0 ? first_slot : 2 * (first_share + p)) * PART; },
         [&](int c, int d, f32x4 o, float m, float l) { write_out<D, T>(a, place(c), d, o, m, l); });
 }

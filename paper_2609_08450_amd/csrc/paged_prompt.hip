@@ -36,8 +36,6 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
     constexpr int KI = kTile * D / 16, KN = (KI + THREADS - 1) / THREADS;  // 16-byte pieces of K, and of a thread
     constexpr int VI = (kTile / 4) * (D / 4), VN = (VI + THREADS - 1) / THREADS;  // 4 x 4 pieces of V
     __shared__ Buffers<D, WAVES> buf[2];
-    __shared__ Joined<THREADS> joined;
-    __shared__ int last;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, g = lane >> 5;
     const int P = 1 << a.lp;
     const int64_t total = a.total[0], shares = a.total[1];
@@ -331,24 +329,13 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
         } else {
             const int first_slot = 2 * s0 + (at == share_start(s0, total, shares) ? 0 : 1);
             float *mine = a.left + (int64_t)(share == s0 ? first_slot : 2 * share) * PART;
-            if (g == 0) give(mine + 2 * col, m, l);
+            if (g == 0) *(f32x2 *)(mine + 2 * col) = f32x2{m, l};
 #pragma unroll
             for (int d = 0; d < D / 32; ++d)
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
-                    give4(mine + 2 * COLS + col * D + 32 * d + 8 * b + 4 * g,
-                          f32x4{o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]} * exp2_(ref));
-            if (arrived_last(&a.tickets[s0], parts, &last)) {
-                join_parts<D, COLS, THREADS>(
-                    joined, parts, min(gr.rows * per_row, COLS),
-                    [&](int p) { return a.left + (int64_t)(p == 0 ? first_slot : 2 * (s0 + p)) * PART; },
-                    [&](int c, int d, f32x4 x, float m2, float l2) {
-                        const int row = c / per_row, h = part * COLS + (c - row * per_row);
-                        if (h < a.per)
-                            write_out<D, T>(a, (int64_t)(gr.row0 + row) * a.heads + kvh * a.per + h, d, x, m2, l2);
-                    });
-            }
-            __syncthreads();
+                    *(f32x4 *)(mine + 2 * COLS + col * D + 32 * d + 8 * b + 4 * g) =
+                        f32x4{o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]} * exp2_(ref);
         }
         left -= end - unit;
         unit = 0;
@@ -363,14 +350,53 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
     }
 }
 
+// Groups that lie in several shares, after prompt_kernel: workgroup = (the share
+// that such a group begins in, 16 of its columns).  (By the last workgroup to
+// arrive instead, four rows over 65000 tokens took 93 us, and one row of 128 heads
+// over 60000 took 392.)
+template <int D, int WAVES, class T>
+__global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
+    constexpr int COLS = 32 * WAVES, PART = COLS * (D + 2);
+    __shared__ Joined<256> joined;
+    const int64_t total = a.total[0], shares = a.total[1];
+    const int w = blockIdx.x, first = 16 * blockIdx.y;
+    if (w + 1 >= shares) return;
+    const int4 st = a.starts[w + 1];
+    if (st.z == 0) return;  // share w + 1 begins with a group
+    const int vheads = a.kv_heads * a.parts, head = st.y;
+    const int gb0 = a.group_base[st.w], gb1 = a.group_base[st.w + 1];
+    const int64_t ru = a.group_units[gb1] - a.group_units[gb0];
+    const int units = a.group_units[st.x + 1] - a.group_units[st.x];
+    const int64_t at = (int64_t)a.group_units[gb0] * vheads + head * ru + (a.group_units[st.x] - a.group_units[gb0]);
+    const int s0 = share_of(at, total, shares), s1 = share_of(at + units - 1, total, shares);
+    if (s0 != w) return;  // it began earlier
+    const Group gr = a.groups[st.x];
+    const int per_row = min(a.per, COLS), cols = min(gr.rows * per_row, COLS);
+    if (first >= cols) return;
+    const int kvh = head / a.parts, part = head - kvh * a.parts;
+    const int first_slot = 2 * s0 + (at == share_start(s0, total, shares) ? 0 : 1);
+    join_parts<D, COLS, 256>(
+        joined, s1 - s0 + 1, first, min(first + 16, cols),
+        [&](int p) { return a.left + (int64_t)(p == 0 ? first_slot : 2 * (s0 + p)) * PART; },
+        [&](int c, int d, f32x4 x, float m, float l) {
+            const int row = c / per_row, h = part * COLS + (c - row * per_row);
+            if (h < a.per)
+                write_out<D, T>(a, (int64_t)(gr.row0 + row) * a.heads + kvh * a.per + h, d, x, m, l);
+        });
+}
+
 template <int D, int WAVES>
 int launch_dim(const AttendArgs &a, int act, int code, int grid, void *stream) {
     const dim3 g((unsigned)grid), b(64 * WAVES);
-    if (code == PAGED_KV_E4M3)
-        return act == PAGED_KV_BF16 ? launch(prompt_kernel<D, WAVES, bf16, E4M3>, g, b, stream, a)
-                                    : launch(prompt_kernel<D, WAVES, f16, E4M3>, g, b, stream, a);
-    return act == PAGED_KV_BF16 ? launch(prompt_kernel<D, WAVES, bf16, Int8>, g, b, stream, a)
-                                : launch(prompt_kernel<D, WAVES, f16, Int8>, g, b, stream, a);
+    const auto go = [&](void (*kernel)(AttendArgs)) { return launch(kernel, g, b, stream, a); };
+    const int rc = code == PAGED_KV_E4M3 ? go(act == PAGED_KV_BF16 ? prompt_kernel<D, WAVES, bf16, E4M3>
+                                                                   : prompt_kernel<D, WAVES, f16, E4M3>)
+                                         : go(act == PAGED_KV_BF16 ? prompt_kernel<D, WAVES, bf16, Int8>
+                                                                   : prompt_kernel<D, WAVES, f16, Int8>);
+    if (rc != PAGED_KV_OK || grid < 2) return rc;
+    const dim3 joins((unsigned)(grid - 1), 2 * WAVES);
+    return act == PAGED_KV_BF16 ? launch(join_kernel<D, WAVES, bf16>, joins, dim3(256), stream, a)
+                                : launch(join_kernel<D, WAVES, f16>, joins, dim3(256), stream, a);
 }
 
 }  // namespace
