@@ -107,7 +107,8 @@ struct Joined {
     float m[BLOCK], l[BLOCK];
 };
 
-template <int D, int COLS, int BLOCK, class Part, class Out>
+// LIVE: the parts were written by workgroups of this launch.
+template <int D, int COLS, int BLOCK, bool LIVE, class Part, class Out>
 __device__ void join_parts(Joined<BLOCK> &j, int parts, int first, int cols, Part part, Out out) {
     constexpr int PER = BLOCK / (D / 4), AHEAD = 8;  // columns of a pass
     const int tid = threadIdx.x, d = tid % (D / 4) * 4;
@@ -125,8 +126,9 @@ __device__ void join_parts(Joined<BLOCK> &j, int parts, int first, int cols, Par
 #pragma unroll
                 for (int i = 0; i < AHEAD; ++i) {
                     const float *from = part(min(p0 + i * spans, parts - 1));
-                    ml[i] = taken(from + 2 * col);
-                    v[i] = taken4(from + 2 * COLS + col * D + d);
+                    const float *values = from + 2 * COLS + col * D + d;
+                    ml[i] = LIVE ? taken(from + 2 * col) : *(const f32x2 *)(from + 2 * col);
+                    v[i] = LIVE ? taken4(values) : *(const f32x4 *)values;
                 }
                 float to = m;
 #pragma unroll
@@ -198,7 +200,7 @@ __device__ void finish(const AttendArgs &a, float (*red)[D + 4], float *top, flo
     for (int c = tid; c < cols; c += BLOCK) give(mine + 2 * c, top[c], sum[c]);
     if (!arrived_last(&a.tickets[first_share], parts, &last)) return;
     // part p lies in slot 0 of share first_share + p, the first one in first_slot
-    join_parts<D, COLS, BLOCK>(
+    join_parts<D, COLS, BLOCK, true>(
         joined, parts, 0, cols,
         [&](int p) { return a.left + (int64_t)(p == 0 ? first_slot : 2 * (first_share + p)) * PART; },
         [&](int c, int d, f32x4 o, float m, float l) { write_out<D, T>(a, place(c), d, o, m, l); });

