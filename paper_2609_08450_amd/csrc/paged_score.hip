@@ -15,6 +15,7 @@
 // 3.4 TB/s of writes, at the card's power limit; 64 rows of 16384 to 131072 tokens
 // 66.6 us, 4.6 TB/s.
 #include "paged_common.h"
+#include "paged_score_plan.h"
 
 namespace paged {
 namespace {
@@ -110,10 +111,6 @@ __device__ void put(float *to, const float (&x)[NT], float scale, int left) {
     for (int t = 0; t < NT; ++t)
         if (t < left) to[t] = scale == -__builtin_inff() ? scale : x[t] * scale;
 }
-
-// Query rows x heads that a workgroup holds, and query rows where every product
-// row is one (their lengths and places).
-constexpr int window_of(int dim) { return dim == 64 ? 512 : 256; }
 
 // Windows of rows: workgroup = (`window` rows, every gridDim.y-th of the blocks of
 // 4 waves x 32 NT tokens).  The queries stay in LDS, each wave passes its own
@@ -336,6 +333,7 @@ int launch_heads(const ScoreArgs &a, dim3 grid, void *stream) {
     const auto go = [&](void (*row)(ScoreArgs), void (*block)(ScoreArgs)) {
         return launch(a.window == 1 ? row : block, grid, dim3(kBlock), stream, a);
     };
+    // the first of these is product_heads(a.heads)
     if (a.heads == 1) return go(score_row_kernel<D, 1, T, C>, score_block_kernel<D, 1, false, T, C>);
     if (a.heads == 2) return go(score_row_kernel<D, 2, T, C>, score_block_kernel<D, 2, false, T, C>);
     if (a.heads <= 4) return go(score_row_kernel<D, 4, T, C>, score_block_kernel<D, 4, false, T, C>);
@@ -382,8 +380,7 @@ extern "C" int paged_kv_score(const paged_kv_cache *cache, int32_t act, const vo
     if (n_rows > n_requests || n_rows > 65535) {
         // rows share their keys: as many to a workgroup as its LDS holds, and so
         // many workgroups to a window as give the card 1024 (2 to a CU are resident)
-        const int hp = heads > 8 ? (heads + 15) / 16 * 16 : heads > 4 ? 8 : heads > 2 ? 4 : heads;
-        a.window = window_of(cache->head_dim) / hp;
+        a.window = rows_of_window(cache->head_dim, heads);
         const int64_t windows = ((int64_t)n_rows + a.window - 1) / a.window;
         const int64_t blocks = (cap + tokens - 1) / tokens, want = (1024 + windows - 1) / windows;
         grid = dim3((unsigned)windows, (unsigned)(want < blocks ? want : blocks));

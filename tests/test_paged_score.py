@@ -50,6 +50,13 @@ def test_single_tokens_and_prompts(code, act, dim, heads):
     check(Setup([300, 64, 1, 200], [300, 5, 1, 37], page=64, **kw), where="prompts")
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("heads", [33, 40, 48, 49, 64, 65, 80, 81, 96, 112, 128])
+def test_prompts_of_many_heads(dim, heads):
+    """Head counts of three to eight products: windows of a few rows, full ones and a rest."""
+    check(Setup([300, 64, 1, 9], [61, 5, 1, 8], page=32, kv=1, heads=heads, dim=dim, values=False), where="many heads")
+
+
 @pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
 def test_pages(page):
     check(Setup([5000, 17], [1, 1], page=page, kv=1, heads=8, dim=64, values=False), where="page")
