@@ -144,7 +144,9 @@ class PagedCache:
     ``k_scale``, ``v_scale`` float32 [n_pages, n_heads].  Pages may be strided
     along the first axis (a layer's slice of [n_pages, layers, ...]).  Calls
     that overlap on different streams each need a workspace of their own
-    (``workspace=``, from ``alloc_workspace``).
+    (``workspace=``, from ``alloc_workspace``).  A workspace that a larger one
+    replaces stays allocated as long as the cache: graphs that were captured
+    with it remain valid.
     """
 
     def __init__(self, n_pages: int, page: int, n_heads: int, head_dim: int,
@@ -192,7 +194,7 @@ class PagedCache:
                          self.n_pages, self.page, self.n_heads, self.head_dim, CODES[k.dtype])
         self._ref = ctypes.byref(self._c)
         self._sizes = {}
-        self.workspace = None
+        self.workspace, self._replaced = None, []
 
     def workspace_size(self, n_rows: int, n_requests: int, heads: int) -> int:
         key = (n_rows, n_requests, heads)
@@ -208,11 +210,13 @@ class PagedCache:
 
     def alloc_workspace(self, n_rows: int, n_requests: int, heads: int, stream=None) -> torch.Tensor:
         """A workspace for attention calls of these sizes, ready for its first use on `stream`."""
+        return self._ready(self.workspace_size(n_rows, n_requests, heads), stream)
+
+    def _ready(self, size, stream):
         if stream is not None and not isinstance(stream, torch.cuda.Stream):
             stream = torch.cuda.ExternalStream(_topk._stream(stream))
         with torch.cuda.stream(stream):
-            ws = torch.empty(self.workspace_size(n_rows, n_requests, heads), dtype=torch.uint8,
-                             device=self.k.device)
+            ws = torch.empty(size, dtype=torch.uint8, device=self.k.device)
             ws[:WORKSPACE_ZEROED].zero_()
         return ws
 
@@ -220,7 +224,12 @@ class PagedCache:
         need = self.workspace_size(n_rows, n_requests, heads)
         if workspace is None:
             if self.workspace is None or self.workspace.numel() < need:
-                self.workspace = self.alloc_workspace(n_rows, n_requests, heads, stream)
+                # A captured graph, or a kernel on another stream, may still use the one
+                # that is replaced, so it stays.  The new one has room to spare (an eighth
+                # more), so that growing sizes replace it seldom.
+                if self.workspace is not None:
+                    self._replaced.append(self.workspace)
+                self.workspace = self._ready(need + max(need // 8, 1 << 20), stream)
             workspace = self.workspace
         elif workspace.dtype is not torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
             raise PagedError("workspace must be a contiguous device tensor of uint8")
