@@ -136,6 +136,13 @@ def _table(table, n=None):
     return table.data_ptr(), stride, width
 
 
+def _on(stream):
+    """The context in which torch allocates and works on `stream` (a handle too; None: the current one)."""
+    if stream is not None and not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_topk._stream(stream))
+    return torch.cuda.stream(stream)
+
+
 class PagedCache:
     """Pages of keys (and values) in 8 bits with their scales, and the workspace of
     the attention calls on them.
@@ -146,7 +153,8 @@ class PagedCache:
     that overlap on different streams each need a workspace of their own
     (``workspace=``, from ``alloc_workspace``).  A workspace that a larger one
     replaces stays allocated as long as the cache: graphs that were captured
-    with it remain valid.
+    with it remain valid.  A captured call needs one of its size already: from a
+    call before the capture, or its own.
     """
 
     def __init__(self, n_pages: int, page: int, n_heads: int, head_dim: int,
@@ -212,10 +220,11 @@ class PagedCache:
         """A workspace for attention calls of these sizes, ready for its first use on `stream`."""
         return self._ready(self.workspace_size(n_rows, n_requests, heads), stream)
 
-    def _ready(self, size, stream):
-        if stream is not None and not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(_topk._stream(stream))
-        with torch.cuda.stream(stream):
+    def _ready(self, size, stream, captured=True):
+        with _on(stream):
+            if not captured and torch.cuda.is_current_stream_capturing():
+                raise PagedError("a cache makes its workspace outside of a capture: make a call of these sizes "
+                                 "before it, or pass workspace=")
             ws = torch.empty(size, dtype=torch.uint8, device=self.k.device)
             ws[:WORKSPACE_ZEROED].zero_()
         return ws
@@ -226,10 +235,12 @@ class PagedCache:
             if self.workspace is None or self.workspace.numel() < need:
                 # A captured graph, or a kernel on another stream, may still use the one
                 # that is replaced, so it stays.  The new one has room to spare (an eighth
-                # more), so that growing sizes replace it seldom.
+                # more), so that growing sizes replace it seldom.  None is made under
+                # capture: it would be the graph's memory, and zeroed by the replays alone.
+                made = self._ready(need + max(need // 8, 1 << 20), stream, captured=False)
                 if self.workspace is not None:
                     self._replaced.append(self.workspace)
-                self.workspace = self._ready(need + max(need // 8, 1 << 20), stream)
+                self.workspace = made
             workspace = self.workspace
         elif workspace.dtype is not torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
             raise PagedError("workspace must be a contiguous device tensor of uint8")

@@ -11,6 +11,7 @@ from tests.paged_util import Setup, assert_attention, attention
 def bare(paged, monkeypatch, sizes):
     """A cache on the CPU whose calls need sizes[n_rows] bytes."""
     monkeypatch.setattr(paged.PagedCache, "workspace_size", lambda self, rows, requests, heads: sizes[rows])
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     cache = paged.PagedCache.__new__(paged.PagedCache)
     cache.k, cache.workspace, cache._replaced = torch.zeros(1), None, []
     return cache
@@ -69,3 +70,41 @@ def test_a_graph_outlives_its_caches_workspace():
         assert all(bool((x == 0x7B).all()) for x in filled)
         assert_attention(out, None, ref, f"replay {i}")
         del filled
+
+
+@pytest.mark.gpu
+def test_no_workspace_is_made_under_capture():
+    """It would be zeroed by the replays alone, and be the graph's memory: calls before
+    the first replay would find tickets that are not zero."""
+    from paper_2609_08450_amd import paged
+
+    s = Setup([9000, 200], [1, 1], page=32, kv=2, heads=8, dim=128).cuda()
+    cache, out, x = s.cache(), torch.empty_like(s.q), torch.zeros(8, device="cuda")
+    args = (s.table, s.row_starts, s.row_lengths, s.scale)
+    side = torch.cuda.Stream()
+    for stream in (None, side, side.cuda_stream):  # the capturing stream is the current one, or given
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            x.add_(1.0)
+            with pytest.raises(paged.PagedError, match="capture"):
+                paged.attend(cache, s.q, *args, out=out, stream=stream)
+            x.add_(1.0)
+        assert cache.workspace is None
+    graph.replay()
+    ref = attention(s)
+    paged.attend(cache, s.q, *args, out=out)
+    torch.cuda.synchronize()
+    assert_attention(out, None, ref, "after a refused capture")
+    # a larger one neither; what fits the one that is there is captured
+    big = Setup([600], [500], page=32, kv=2, heads=8, dim=128).cuda()
+    had, graph = cache.workspace, torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(paged.PagedError, match="capture"):
+            paged.attend(cache, big.q, s.table[:1], big.row_starts, big.row_lengths, s.scale)
+        paged.attend(cache, s.q, *args, out=out)
+    assert cache.workspace is had
+    for i in range(3):
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert_attention(out, None, ref, f"replay {i}")
