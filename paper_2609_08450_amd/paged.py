@@ -9,6 +9,10 @@ As in ``topk``, every function checks and marshals arguments and forwards
 device pointers and the stream to the library (libpaged_kv.so); all work runs
 in its HIP kernels, there is no fallback.  include/paged_kv.h holds the
 contract of each call.
+
+``stream`` (a torch stream or a handle; None: the current one) is where a call
+runs.  Inputs have to be ready there, and an output that a call makes belongs to
+that stream, as if torch had made it there.
 """
 from __future__ import annotations
 
@@ -280,9 +284,12 @@ def store(cache: PagedCache, k_new, v_new, slots, stream=None) -> None:
            "paged_kv_store")
 
 
-def _outputs(cache, q, out, lse):
-    if out is None:
+def _outputs(q, out, lse, stream):
+    if out is None and stream is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif out is None:  # of the stream that writes it: its memory may still be in use on the current one
+        with _on(stream):
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     at = _ptr(out, q.dtype, q.shape, "out")
     return out, at, _ptr(lse, torch.float32, q.shape[:2], "lse") if lse is not None else None
 
@@ -295,7 +302,7 @@ def attend(cache: PagedCache, q, table, row_starts, row_lengths, scale: float, o
     rows, heads, _ = q.shape
     at, stride, width = _table(table)
     n = table.shape[0]
-    out, op, lp = _outputs(cache, q, out, lse)
+    out, op, lp = _outputs(q, out, lse, stream)
     ws, size = cache._space(workspace, rows, n, heads, stream)
     _check((_lib or lib()).paged_kv_attend(
         cache._ref, ACTS[q.dtype], qp, q_row, q_head, heads, at, stride, width,
@@ -313,7 +320,7 @@ def attend_selected(cache: PagedCache, q, idx, table, row_request, row_lengths, 
     rows, heads, _ = q.shape
     at, stride, width = _table(table)
     n = table.shape[0]
-    out, op, lp = _outputs(cache, q, out, lse)
+    out, op, lp = _outputs(q, out, lse, stream)
     ws, size = cache._space(workspace, rows, n, heads, stream)
     _check((_lib or lib()).paged_kv_attend_selected(
         cache._ref, ACTS[q.dtype], qp, q_row, q_head, heads, _ptr(idx, torch.int32, (rows, None), "idx"),
