@@ -43,8 +43,10 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
     const int P = 1 << a.lp;
     const int64_t total = a.total[0], shares = a.total[1];
 
-    // rows that no request has
-    for (int64_t i = max(a.row_starts[a.n_requests], 0) + (int64_t)blockIdx.x; i < a.n_rows; i += gridDim.x) {
+    // rows that no request has: before the first one's, and past the last one's
+    const int lead = min(max(a.row_starts[0], 0), a.n_rows), past = max(a.row_starts[a.n_requests], lead);
+    for (int64_t j = blockIdx.x; j < (int64_t)lead + max(a.n_rows - past, 0); j += gridDim.x) {
+        const int64_t i = j < lead ? j : past + (j - lead);
         for (int e = tid; e < a.heads * D / 2; e += THREADS) ((u32 *)a.out)[i * a.heads * D / 2 + e] = 0;
         if (a.lse)
             for (int e = tid; e < a.heads; e += THREADS) a.lse[i * a.heads + e] = -__builtin_inff();

@@ -128,6 +128,34 @@ def test_rows_of_no_request(prompt):
     assert bool((out[int(s.row_starts[2]):] == 0).all()) and bool((lse[int(s.row_starts[2]):] == -torch.inf).all())
 
 
+@pytest.mark.parametrize("before,rows,after", [(1, [1, 1], 0), (2, [1, 0, 1], 2), (3, [4, 5], 0), (3, [4, 0, 5], 2),
+                                               (700, [40, 3], 300)])
+def test_rows_before_the_first_request(before, rows, after):
+    """row_starts begins after the rows do: single rows and prompts."""
+    s = Setup([50 + i for i in range(len(rows))], rows, dim=64)
+    n = s.n_rows
+    s.q = torch.cat([s.q[:1].repeat(before, 1, 1), s.q, s.q[:1].repeat(after, 1, 1)])
+    s.row_lengths = torch.cat([torch.full((before,), 9, dtype=torch.int32), s.row_lengths,
+                               torch.full((after,), 9, dtype=torch.int32)])
+    s.row_request = torch.cat([torch.full((before,), -1, dtype=torch.int32), s.row_request])
+    s.row_starts += before
+    s.n_rows += before + after
+    out, lse = check(s, where="rows before")
+    for part in (slice(0, before), slice(before + n, None)):
+        assert bool((out[part] == 0).all()) and bool((lse[part] == -torch.inf).all())
+
+
+def test_rows_of_no_requests_at_all():
+    from paper_2609_08450_amd import paged
+
+    s = Setup([50], [5], dim=64).cuda()
+    for start in (0, 2, 5, 9):
+        out, lse = torch.full_like(s.q, 7.0), torch.full((5, 8), 7.0, device="cuda")
+        paged.attend(s.cache(), s.q, s.table[:0], torch.tensor([start], dtype=torch.int32).cuda(), s.row_lengths, s.scale,
+                     out=out, lse=lse)
+        assert bool((out == 0).all()) and bool((lse == -torch.inf).all())
+
+
 @pytest.mark.parametrize("prompt", [False, True])
 def test_pages_outside_the_cache_are_absent(prompt):
     s = Setup([200, 90, 33], [1, 1, 1] if not prompt else [150, 20, 3], page=16, dim=64)
