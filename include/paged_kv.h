@@ -87,7 +87,8 @@ typedef struct paged_kv_cache {
  * request's pages are left as they are.  Rows past the last request's have
  * request -1, length 0 and slot -1; rows that do not fit n_rows are not
  * written (row_starts still counts them).
- * pool_out may be pool_in and lens_out may be lens_in. */
+ * pool_out may be pool_in.  lens_out may not be lens_in (EINVAL): the rows are
+ * made from the lengths before the step and from those after it. */
 int paged_kv_tables(int32_t *ring, int32_t ring_size, const int32_t *pool_in, int32_t *pool_out,
                     const int32_t *lens_in, const int32_t *new_lens, int32_t *lens_out,
                     int32_t n_requests, int32_t *table, int32_t table_stride, int32_t table_width,

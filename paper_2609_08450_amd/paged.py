@@ -255,7 +255,8 @@ def tables(ring, pool, lens, new_lens, table, page: int, *, pool_out, lens_out, 
            row_lengths, slots, stream=None) -> None:
     """Forwards to paged_kv_tables(): a step's block tables, rows and slots from
     request lengths.  ``pool`` int32 [4] (place of the ring's first free page,
-    count, ...); the number of rows is that of ``slots``."""
+    count, ...); the number of rows is that of ``slots``.  ``pool_out`` may be
+    ``pool``; ``lens_out`` is another tensor than ``lens``."""
     n, rows = lens.numel(), slots.numel()
     i32 = torch.int32
     at, stride, width = _table(table, n)

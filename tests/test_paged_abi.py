@@ -119,6 +119,22 @@ def test_tables_arguments(paged):
         assert call(**bad) == EUNSUPPORTED, bad
 
 
+def test_the_header_says_which_tables_arguments_may_be_one(paged):
+    text = " ".join(open(HEADER).read().replace("*", " ").split())
+
+    def call(pool_out, lens_out, n):  # nothing is launched here: without a GPU the last check refuses
+        return paged.lib().paged_kv_tables(4096, 16, 4096, pool_out, 4096, 4096, lens_out, n, 4096, 8, 8, 16, 0, 4096,
+                                           None, None, None, None)
+
+    assert "pool_out may be pool_in." in text and "lens_out may not be lens_in (EINVAL)" in text
+    assert "lens_out may be lens_in" not in text
+    assert call(8192, 4096, 3) == EINVAL
+    import torch
+
+    if not torch.cuda.is_available():
+        assert call(4096, 8192, 3) == EUNSUPPORTED
+
+
 def test_status_texts(paged):
     L = paged.lib()
     assert L.paged_kv_status_str(-1) == b"invalid argument"
