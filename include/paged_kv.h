@@ -86,7 +86,7 @@ typedef struct paged_kv_cache {
  * table_width: its rows have length 0 and slot -1.  Table entries past a
  * request's pages are left as they are.  Rows past the last request's have
  * request -1, length 0 and slot -1; rows that do not fit n_rows are not
- * written (row_starts still counts them).
+ * written (row_starts still counts them, up to 2^31 - 1).
  * pool_out may be pool_in.  lens_out may not be lens_in (EINVAL): the rows are
  * made from the lengths before the step and from those after it. */
 int paged_kv_tables(int32_t *ring, int32_t ring_size, const int32_t *pool_in, int32_t *pool_out,

@@ -80,6 +80,10 @@ __device__ Sums prefix(Sums x, Sums *waves, Sums *all) {
     return {before.give + s.give - x.give, before.take + s.take - x.take, before.rows + s.rows - x.rows};
 }
 
+// Counts of rows past 32 bits stay at the largest: were they to wrap, a row's search in
+// them could end at a request that it does not belong to, outside its table.
+__device__ int held(int64_t rows) { return (int)min(rows, (int64_t)0x7FFFFFFF); }
+
 // Last i in [0, n) with starts[i] <= x (starts rise, starts[0] <= x).
 __device__ int last_start(const int32_t *starts, int n, int x) {
     int lo = 0, hi = n;
@@ -193,7 +197,7 @@ __global__ __launch_bounds__(BLOCK) void tables_kernel(TablesArgs a, bool own) {
         if (no) atomicAdd(&refused, 1);
         if (granted && c.take > 0) atomicMax(&taken, (unsigned long long)upto);
         if (r < a.n) {
-            const int start = (int)(done.rows + at.rows);
+            const int start = held(done.rows + at.rows);
             a.lens_out[r] = (int32_t)(no ? c.len : c.to);
             a.row_starts[r] = start;
             if (own) {
@@ -213,7 +217,7 @@ __global__ __launch_bounds__(BLOCK) void tables_kernel(TablesArgs a, bool own) {
     }
     __syncthreads();
     if (tid == 0) {
-        a.row_starts[a.n] = (int32_t)done.rows;
+        a.row_starts[a.n] = held(done.rows);
         a.pool_out[0] = (int32_t)((head + (int64_t)taken) % size);
         a.pool_out[1] = (int32_t)(free_in + given - (int64_t)taken);
         a.pool_out[2] = refused;

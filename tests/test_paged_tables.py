@@ -92,6 +92,21 @@ def test_released_pages_serve_the_same_step():
     check(*make(2, page, 9, [0, 200], [150, -200], 0, 0), page)
 
 
+@pytest.mark.parametrize("rows", [50, 9000])
+@pytest.mark.parametrize("more", [[], [1] * 2000])
+def test_rows_past_32_bits(rows, more):
+    """Refused requests that ask for more rows than 32 bits count, before one that is served."""
+    page, most = 16, 2 ** 31 - 1
+    lens, new = [0, 0, 20, 0] + [0] * len(more), [most, 2 ** 30, 5, 1] + more
+    print("[case] tables, rows past 32 bits", rows, len(more), flush=True)
+    got = run(*make(len(lens), page, 9, lens, new, 10, 0), page, rows)
+    assert got["row_starts"] == [0] + [most] * len(lens)
+    assert got["row_request"] == [0] * rows and got["row_lengths"] == [0] * rows and got["slots"] == [-1] * rows
+    served = min(10, 1 + len(more))  # pages go to the requests of one token, in order
+    assert got["lens_out"] == [0, 0, 25] + [1] * served + [0] * (1 + len(more) - served)
+    assert got["pool_out"][1:] == [10 - served, 2 + 1 + len(more) - served, 0]
+
+
 def test_no_requests():
     check([3, 1, 2], [1, 2, 0, 0], [], [], [], 16, rows=4)
     check([3, 1, 2], [1, 2, 0, 0], [], [], [], 16, rows=5000)
