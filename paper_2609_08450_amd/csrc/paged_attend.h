@@ -141,8 +141,8 @@ __device__ void join_parts(Joined<BLOCK> &j, int parts, int first, int cols, Par
                 l *= by;
 #pragma unroll
                 for (int i = 0; i < AHEAD; ++i) {
-                    // (a part that saw nothing has no values either)
-                    const float w = ml[i][1] > 0.0f ? exp2_(ml[i][0] - to) : 0.0f;
+                    // (a part that saw nothing has no values either; a sum that is NaN stays one)
+                    const float w = ml[i][1] != 0.0f ? exp2_(ml[i][0] - to) : 0.0f;
                     l += ml[i][1] * w;
                     o += v[i] * w;
                 }

@@ -194,6 +194,26 @@ def test_peaked_and_large_scores():
               where="peaked")
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("lens,rows", [([40, 50], [1, 1]), ([30000, 50], [1, 1]), ([300, 50], [40, 1]), ([9000, 50], [100, 1])])
+def test_queries_that_are_not_finite_show(lens, rows, bad):
+    """A head's NaN is its result, in one part or joined from many, and no other head's."""
+    s = Setup(lens, rows, page=32, kv=2, heads=8, dim=128)
+    s.q[1, 3], s.q[0, 6, 5] = bad, bad
+    s.cuda()
+    hit = torch.zeros((s.n_rows, 8), dtype=torch.bool, device="cuda")
+    hit[1, 3] = hit[0, 6] = True
+    finite = s.q.clone()
+    finite[hit] = 1.0
+    idx = torch.arange(3000, dtype=torch.int32, device="cuda").repeat(s.n_rows, 1)
+    for picked in (None, idx):
+        out, lse = run(s, picked)
+        assert bool(torch.isnan(out[hit]).all()) and bool(torch.isnan(lse[hit]).all())
+        t = Setup.__new__(Setup)
+        vars(t).update(vars(s), q=finite)
+        assert torch.equal(out[~hit], run(t, picked)[0][~hit])
+
+
 # Layouts.
 
 @pytest.mark.parametrize("prompt", [False, True])
