@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kTile = 64;
 constexpr float kNoScale = -200.0f;  // log2 of a scale of 0, near enough: below every scale that a value survives
-constexpr float kFaint = -60.0f;     // values this far (powers of 2) below the reference are 0 in f16 weights
+constexpr float kFaint = -60.0f;     // weights this far (powers of 2) below the maximum's have values of 0 in f16
 
 // Chunk of 16 bytes of V's row d that holds chunk c: reads of 32 rows and writes
 // of every fourth row both spread over the banks.
@@ -29,7 +29,7 @@ template <int D, int WAVES>
 struct Buffers {
     alignas(16) uint8_t k[kTile][2 * D + 16];
     alignas(16) uint8_t v[D][2 * kTile];
-    float kf[4], lv[4];  // of each 16 tokens: the keys' scale, the values' as a power of 2
+    alignas(16) float kf[4], lv[4];  // of each 16 tokens: the keys' scale, the values' as a power of 2
     u32 valid;           // bit of each 16 tokens: its page is in the cache
 };
 
@@ -98,7 +98,11 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
         f32x16 o[D / 32];
         for (int t = 0; t < D / 32; ++t)
             for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
-        float m = kLow, l = 0.0f, ref = kLow;  // values are held over 2^ref
+        // The sum is held over 2^m, values over 2^ref.  `ref` follows the largest product of
+        // weight and scale that the column has seen: f16 weights keep their bits down to
+        // 2^-20 of that one, whatever the scales of pages that weigh nothing or that its
+        // row does not see.
+        float m = kLow, l = 0.0f, ref = kLow;
 
         // Codes on their way: pages a tile ahead of codes, codes a tile ahead of use.
         // Nothing that is loaded is used where it is loaded, not even in a
@@ -202,22 +206,7 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
                 }
                 const int tok0 = kTile * u;
                 if (tok0 < longest) {
-                    const f32x4 kf = *(const f32x4 *)b.kf;
-                    f32x4 lv = *(const f32x4 *)b.lv;
                     const u32 valid = __builtin_amdgcn_readfirstlane(b.valid);
-                    const float vmax = fmaxf(fmaxf(lv[0], lv[1]), fmaxf(lv[2], lv[3]));
-                    if (__any(vmax > ref + 7.0f)) {  // weights stay below 2^(8 + 7) in f16
-                        const float by = exp2_(ref - (vmax - 6.0f));
-#pragma unroll
-                        for (int t = 0; t < D / 32; ++t) o[t] *= by;
-                        ref = vmax - 6.0f;
-                    }
-                    f32x4 back;  // what takes a weight's scale off again, for the sum
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        lv[i] = fmaxf(lv[i] - ref, kFaint);
-                        back[i] = exp2_(-lv[i]);
-                    }
                     const bool all = valid == 15u && tok0 + kTile <= shortest;
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
@@ -250,9 +239,10 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
                         for (int h = 0; h < EARLY; ++h)
 #pragma unroll
                             for (int d = 0; d < D / 32; ++d) vv[h][d] = v_piece(h, d);
+                        const f32x2 kf = *(const f32x2 *)&b.kf[2 * t], lv = *(const f32x2 *)&b.lv[2 * t];
                         __builtin_amdgcn_sched_barrier(0);
-                        // A weight with its value's scale is 2^(s kf + lv - m): one multiply-add and
-                        // one exponential; scales are not negative, so the maximum is taken before them.
+                        // A weight with its value's scale is 2^(s kf + lv - ref): one multiply-add and one
+                        // exponential; scales are not negative, so the maximum is taken before them.
                         u32 gone = 0;
                         if (!all)
 #pragma unroll
@@ -260,31 +250,38 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
                                 const int tok = tok0 + 32 * t + 8 * (i >> 2) + 4 * g + (i & 3);
                                 if (tok >= len || !((valid >> (2 * t + (i >> 3))) & 1)) gone |= 1u << i;
                             }
+                        float x[2];  // of 16 tokens each, in powers of 2
                         const auto highest = [&](auto masked) {
-                            float x[2];
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
                                 x[h] = -__builtin_inff();
 #pragma unroll
                                 for (int i = 8 * h; i < 8 * h + 8; ++i)
                                     x[h] = fmaxf(x[h], decltype(masked)::value && ((gone >> i) & 1) ? -__builtin_inff() : s[i]);
+                                x[h] *= kf[h];  // (NaN of -inf and 0, which the maxima pass over)
                             }
-                            return fmaxf(fmaxf(kLow, x[0] * kf[2 * t]), x[1] * kf[2 * t + 1]);
                         };
-                        float top = all ? highest(std::false_type{}) : highest(std::true_type{});
-                        if (__any(top > m + kSlack)) {
+                        if (all) highest(std::false_type{});
+                        else highest(std::true_type{});
+                        float top = fmaxf(fmaxf(kLow, x[0]), x[1]);
+                        float heavy = fmaxf(x[0] + lv[0], x[1] + lv[1]);
+                        if (__any(top > m + kSlack || heavy > ref + 15.0f)) {  // weights stay below 2^15 in f16
                             top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), m);
-                            const float by = exp2_(m - top);
-                            l *= by;
-#pragma unroll
-                            for (int d = 0; d < D / 32; ++d) o[d] *= by;
+                            l *= exp2_(m - top);
                             m = top;
+                            heavy = fmaxf(heavy, __shfl_xor(heavy, 32));
+                            if (__any(heavy > ref + 15.0f)) {
+                                const float to = fmaxf(heavy - 6.0f, ref), by = exp2_(ref - to);
+#pragma unroll
+                                for (int d = 0; d < D / 32; ++d) o[d] *= by;
+                                ref = to;
+                            }
                         }
                         u32x4 p[2];
                         const auto weigh = [&](auto masked) {
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
-                                const float f = kf[2 * t + h], c = lv[2 * t + h] - m;
+                                const float f = kf[h], c = fmaxf(lv[h] - ref, kFaint - m);
                                 float e[8], sum = 0.0f;
 #pragma unroll
                                 for (int i = 0; i < 8; ++i) {
@@ -294,7 +291,7 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
                                 }
                                 p[h] = u32x4{pack_f16(e[0], e[1]), pack_f16(e[2], e[3]), pack_f16(e[4], e[5]),
                                              pack_f16(e[6], e[7])};
-                                l = fmaf(sum, back[2 * t + h], l);
+                                l = fmaf(sum, exp2_(-m - c), l);  // (the scale off again)
                             }
                         };
                         if (all) weigh(std::false_type{});
@@ -318,8 +315,11 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
         const int64_t ru = a.group_units[gb1] - a.group_units[gb0];
         const int64_t at = (int64_t)a.group_units[gb0] * vheads + head * ru + (a.group_units[gi] - a.group_units[gb0]);
         const int s0 = share_of(at, total, shares), s1 = share_of(at + units - 1, total, shares), parts = s1 - s0 + 1;
+        const float half = exp2_(0.5f * (ref - m));  // twice: this power may lie below FP32's normal numbers where the values do not
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) o[d] *= half;
         if (parts == 1) {
-            const float by = l != 0.0f ? exp2_(ref) / l : 0.0f;
+            const float by = l != 0.0f ? half / l : 0.0f;
             if (out_at >= 0) {
 #pragma unroll
                 for (int d = 0; d < D / 32; ++d)
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(AttendArgs a) {
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
                     *(f32x4 *)(mine + 2 * COLS + col * D + 32 * d + 8 * b + 4 * g) =
-                        f32x4{o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]} * exp2_(ref);
+                        f32x4{o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]} * half;
         }
         left -= end - unit;
         unit = 0;

@@ -11,8 +11,9 @@
 // bytes are brought to it by 4 x 4 byte transposes.  No value crosses lanes
 // but the maximum, and that only when it moves by more than 2^8.
 // P is rounded to f16 (11 bits, whatever q's type: V's codes are exact in it),
-// weighted with V's scale over a reference that follows the largest one seen so
-// far, so that its range does not depend on the scales.
+// weighted with V's scale over a reference of each column's own that follows the
+// largest product of weight and scale seen so far: full bits down to 2^-20 of that
+// product, whatever the scales of pages that weigh nothing.
 // Measured (heads of 128, e4m3): 64 rows of 16384 to 131072 tokens 396 us, 5.83
 // TB/s; one row of 131071 tokens on 8 heads 57 us; 4096 rows of 2048 selected
 // tokens 266 us, 8.1 TB/s of gathers out of the last-level cache.
@@ -24,6 +25,8 @@ namespace {
 constexpr int kBlock = 256;
 constexpr int kUnit = 128;     // tokens: 32 to a wave
 constexpr int kSliceRows = kStreamRows;
+constexpr float kLeastRef = 0x1p-120f;  // of a reference: one over it is finite
+constexpr float kMostWeight = 32768.0f; // of a weight in f16
 
 // 32 tokens' codes of one lane.
 template <int D>
@@ -51,33 +54,20 @@ struct Wave {
     typename Act<T>::frag q[NT][D / 32];
     f32x4 o[NT][D / 16];
     float m[NT], l[NT];
-    float ref, inv;  // values are held over `ref`
+    float ref[NT], inv[NT];  // values are held over `ref`, and inv = 1 / ref
 
     __device__ void clear() {
         for (int t = 0; t < NT; ++t) {
             m[t] = kLow;
             l[t] = 0.0f;
+            ref[t] = kLeastRef;
+            inv[t] = 1.0f / kLeastRef;
             for (int j = 0; j < D / 16; ++j) o[t][j] = f32x4{0, 0, 0, 0};
-        }
-        ref = 0.0f;
-        inv = 0.0f;
-    }
-
-    // Before tokens whose largest scale is vs (the same in all lanes): f16 weights are
-    // then at most 2^8 (a maximum's slack) * 2^7, and exact to 11 bits down to 2^-20.
-    __device__ bool beyond(float vs) const { return vs > 128.0f * ref; }
-    __device__ void reference(float vs) {
-        if (beyond(vs)) {
-            const float to = vs * 0.015625f, by = ref / to;
-            for (int t = 0; t < NT; ++t)
-                for (int j = 0; j < D / 16; ++j) o[t][j] *= by;
-            ref = to;
-            inv = 1.0f / to;
         }
     }
 
     // seen: bit 4 a + i says whether token 16 a + 4 g + i is there; kf, vf: scales
-    // of those tokens, the keys' times scale * log2(e), the values' over ref.
+    // of those tokens, the keys' times scale * log2(e).
     __device__ void take(const Tile<D> &x, u32 seen, bool all, const float (&kf)[2][4], const float (&vf)[2][4]) {
         f32x4 s[NT][2];
 #pragma unroll
@@ -109,23 +99,55 @@ struct Wave {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
                 top = fmaxf(top, m[t]);
-                const float by = exp2_(m[t] - top);
+                const float by = exp2_(m[t] - top), to = ref[t] * by;
                 l[t] *= by;
-#pragma unroll
-                for (int j = 0; j < D / 16; ++j) o[t][j] *= by;
                 m[t] = top;
+                // the values so far weigh less: so does what they are held over
+                if (__any(to < kLeastRef)) {
+                    const float left = fminf(to * (1.0f / kLeastRef), 1.0f);
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j) o[t][j] *= left;
+                }
+                ref[t] = fmaxf(to, kLeastRef);
+                inv[t] = __builtin_amdgcn_rcpf(ref[t]);
             }
-            float e[2][4];
+            float e[2][4], w[2][4], most = 0.0f;
+            const auto weigh = [&] {
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[a][i] = e[a][i] * fminf(vf[a][i] * inv[t], 3e38f);  // (finite: 0 stays 0)
+            };
 #pragma unroll
             for (int a = 0; a < 2; ++a)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     e[a][i] = exp2_(s[t][a][i] - m[t]);
                     l[t] += e[a][i];
-                    e[a][i] *= vf[a][i];
                 }
-            p[t] = u32x4{pack_f16(e[0][0], e[0][1]), pack_f16(e[0][2], e[0][3]), pack_f16(e[1][0], e[1][1]),
-                         pack_f16(e[1][2], e[1][3])};
+            weigh();
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) most = fmaxf(most, w[a][i]);
+            if (__any(most > kMostWeight)) {  // it is 2^6 then
+                float to = 0.0f;
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) to = fmaxf(to, e[a][i] * vf[a][i]);
+                to = fmaxf(to, __shfl_xor(to, 16));
+                to = fmaxf(to, __shfl_xor(to, 32));
+                to = fmaxf(to * 0.015625f, ref[t]);
+                const float by = ref[t] * __builtin_amdgcn_rcpf(to);
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) o[t][j] *= by;
+                ref[t] = to;
+                inv[t] = __builtin_amdgcn_rcpf(to);
+                weigh();
+            }
+            p[t] = u32x4{pack_f16(w[0][0], w[0][1]), pack_f16(w[0][2], w[0][3]), pack_f16(w[1][0], w[1][1]),
+                         pack_f16(w[1][2], w[1][3])};
         }
 #pragma unroll
         for (int w = 0; w < D / 64; ++w) {
@@ -177,7 +199,7 @@ __device__ void join_waves(Wave<D, NT, T, C> &w, Shared<D, NT> &sh) {
         const int c = 16 * t + n;
         float m = sh.top[0][c];
         for (int i = 1; i < 4; ++i) m = fmaxf(m, sh.top[i][c]);
-        by[t] = exp2_(w.m[t] - m) * w.ref;
+        by[t] = exp2_(w.m[t] - m) * w.ref[t];
         if (wave == 0 && g == 0) {
             float l = 0.0f;
             for (int i = 0; i < 4; ++i) l += sh.sum[i][c] * exp2_(sh.top[i][c] - m);
@@ -360,9 +382,6 @@ __global__ __launch_bounds__(kBlock, D * NT <= 128 ? 2 : 1) void stream_kernel(A
             }
         };
         const auto take = [&](const Tile<D> &x, int lim0, int lim1, float k0, float k1, float v0, float v1) {
-            w.reference(fmaxf(v0, v1));
-            v0 *= w.inv;
-            v1 *= w.inv;
             const float kf[2][4] = {{k0, k0, k0, k0}, {k1, k1, k1, k1}};
             const float vf[2][4] = {{v0, v0, v0, v0}, {v1, v1, v1, v1}};
             const bool all = lim0 >= 16 && lim1 >= 16;
@@ -472,7 +491,7 @@ __global__ __launch_bounds__(kBlock, D * NT <= 128 ? 2 : 1) void selected_kernel
             for (int e = 0; e < 4; ++e) {
                 seen |= (r[e] != ~0u ? 1u : 0u) << (4 * h + e);
                 k2[h][e] = ks[e];
-                v2[h][e] = vs[e] * w.inv;
+                v2[h][e] = vs[e];
             }
         }
         if (__all(seen == 0xFF)) w.take(x, 0xFF, true, k2, v2);
@@ -480,12 +499,7 @@ __global__ __launch_bounds__(kBlock, D * NT <= 128 ? 2 : 1) void selected_kernel
     };
     const auto put_scales = [&](int at, bool there, float ks, float vs) {
         kf[wave][at][lane] = there ? ks * a.scale2 : 0.0f;
-        vs = there ? vs : 0.0f;
-        vf[wave][at][lane] = vs;
-        if (__any(w.beyond(vs))) {
-            for (int d = 32; d; d >>= 1) vs = fmaxf(vs, __shfl_xor(vs, d));
-            w.reference(vs);
-        }
+        vf[wave][at][lane] = there ? vs : 0.0f;
         __builtin_amdgcn_wave_barrier();
     };
     if (first < stop) {

@@ -194,6 +194,95 @@ def test_peaked_and_large_scores():
               where="peaked")
 
 
+def far_scales(lens, rows, ratio, where, code, act, dim=128, heads=8, seen=None):
+    """Pages `where` of each request have values 2^ratio times as large as the others,
+    and keys that queries of one sign do not look at (a weight of about e^-80) while
+    those of the other sign look at nothing else."""
+    s = Setup(lens, rows, page=16, kv=2, heads=heads, dim=dim, code=code, act=act, seen=seen)
+    g = torch.Generator().manual_seed(ratio)
+    shift = torch.full((s.n_pages, 1, 1, 1), 0.5)
+    s.vs[:] = 2.0 ** -6
+    for t in s.table.tolist():
+        for j in where:
+            if j < len(t) and t[j] >= 0:
+                shift[t[j]] = -0.5
+                s.vs[t[j]] = 2.0 ** (ratio - 6)
+    k = 0.05 * torch.randn(s.k.shape, generator=g) + shift
+    s.ks[:] = 1 / 64
+    s.k = (k * 64).round().to(code) if code is torch.int8 else (k * 64).to(code)
+    sign = 1 - 2 * torch.randint(0, 2, (s.n_rows, heads, 1), generator=g)
+    sign[::3] = 1  # most look at the others
+    s.q = ((7 * sign + 0.3 * torch.randn(s.q.shape, generator=g)) * (128 / dim) ** 0.5).to(act)
+    return s
+
+
+def check_far(s, picked=None):
+    """Each row and head against its own mass.  Weights are rounded to f16 and follow
+    scores that FP32 holds (a part in 2^24 for each of the products); a weight below f16's
+    normal ones is off by 2^-25 of a unit that is at most 2^-6 of the row's largest product of weight and
+    scale, which is at most the sum of them (the mass of values of 1)."""
+    s.cuda()
+    out, lse = run(s, picked)
+    ref, ref_lse, mass = attention(s, picked)
+    one = Setup.__new__(Setup)
+    vars(one).update(vars(s), v=torch.ones_like(s.v.float()).to(s.v.dtype))
+    weighed = attention(one, picked)[0]
+    tokens = int(s.row_lengths.max()) if picked is None else picked.shape[1]
+    unit, least = (2.0 ** -8, 2.0 ** -133) if s.act is torch.bfloat16 else (2.0 ** -11, 2.0 ** -25)
+    empty = ref_lse == -torch.inf
+    score = s.dim * 2.0 ** -24 * float(ref_lse[~empty].abs().max())
+    tol = unit * ref.abs() + (2.0 ** -10 + 2 * score) * mass + tokens * 448 * 2.0 ** -31 * weighed + least
+    off = (out.double() - ref).abs()
+    over = ref.abs() + tol > torch.finfo(s.act).max  # past f16's largest
+    bad = (off > tol) & ~over
+    assert not bool(bad.any()), (f"{int(bad.sum())} of {bad.numel()} out of bounds, first at {bad.nonzero()[0].tolist()}: "
+                                 f"{float(out[bad][0])} for {float(ref[bad][0])}")
+    assert bool((lse[empty] == -torch.inf).all()) and bool((out[empty] == 0).all())
+    assert bool(((lse.double() - ref_lse)[~empty].abs() <= 2.0 ** -15 * (1 + ref_lse[~empty].abs())).all())
+
+
+@pytest.mark.parametrize("code", CODE, ids=str)
+@pytest.mark.parametrize("act", ACT, ids=str)
+@pytest.mark.parametrize("ratio", [-40, 8, 16, 22, 30, 50])
+@pytest.mark.parametrize("lens,rows,where", [([600, 50], [1, 1], [0]), ([600, 50], [1, 1], [3, 20]), ([600], [1], [36]),
+                                             ([600, 90], [60, 5], [0, 1]), ([600, 90], [600, 90], [2, 17, 30])])
+def test_pages_that_weigh_nothing_cost_no_precision(code, act, ratio, lens, rows, where):
+    """However large their values, and whether other rows look at them or see them."""
+    print("[case] far scales", lens, rows, where, ratio, code, act, flush=True)
+    s = far_scales(lens, rows, ratio, where, code, act)
+    idx = selection(s, 300)
+    check_far(s)
+    check_far(s, idx)
+
+
+@pytest.mark.parametrize("dim,heads", [(64, 8), (256, 8), (128, 40), (64, 66)])
+@pytest.mark.parametrize("rows", [[1, 1], [200, 30]])
+def test_far_scales_of_other_heads(dim, heads, rows):
+    s = far_scales([600, 50], rows, 30, [0, 9], torch.float8_e4m3fn, torch.bfloat16, dim=dim, heads=heads)
+    idx = selection(s, 300)
+    check_far(s)
+    check_far(s, idx)
+
+
+def test_rows_that_do_not_see_the_large_values():
+    """In prompts: pages that only later rows of the group see."""
+    seen = [100, 100, 600, 600, 90, 33, 17, 600] * 5
+    s = far_scales([600], [40], 40, [8, 9, 30], torch.float8_e4m3fn, torch.float16, seen=seen)
+    check_far(s)
+
+
+def test_zero_scales_beside_others():
+    """Pages of scale 0 (and keys' scales of 0) hold weight but no values."""
+    for rows in ([1, 1], [60, 20]):
+        s = far_scales([600, 50], rows, 0, [0, 1, 9], torch.float8_e4m3fn, torch.bfloat16)
+        g = torch.Generator().manual_seed(5)
+        s.vs[torch.rand(s.vs.shape, generator=g) < 0.4] = 0.0
+        s.ks[torch.rand(s.ks.shape, generator=g) < 0.2] = 0.0
+        idx = selection(s, 300)
+        check_far(s)
+        check_far(s, idx)
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 @pytest.mark.parametrize("lens,rows", [([40, 50], [1, 1]), ([30000, 50], [1, 1]), ([300, 50], [40, 1]), ([9000, 50], [100, 1])])
 def test_queries_that_are_not_finite_show(lens, rows, bad):
