@@ -87,10 +87,29 @@ def _check(rc: int, what: str):
         raise PagedError(f"{what} failed: {lib().paged_kv_status_str(rc).decode()} ({rc})")
 
 
-def _ptr(t, dtype, shape, name):
-    """Address of a contiguous device tensor of this type and shape (None: any size)."""
-    if not t.is_cuda:
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _device(t, name):
+    """The device of a call: its first tensor's, which has to be the current one (launches go there)."""
+    dev = t.get_device()
+    if dev < 0:
         raise PagedError(f"{name} must be a device tensor")
+    if dev != _current_device():
+        raise PagedError(f"{name} is on cuda:{dev}, but the current device is cuda:{_current_device()}")
+    return dev
+
+
+def _elsewhere(t, dev, name):
+    if t.get_device() < 0:
+        return PagedError(f"{name} must be a device tensor")
+    return PagedError(f"{name} is on cuda:{t.get_device()}, the call's other tensors are on cuda:{dev}")
+
+
+def _ptr(t, dtype, shape, name, dev):
+    """Address of a contiguous tensor of this type and shape (None: any size) on device `dev`."""
+    if t.get_device() != dev:
+        raise _elsewhere(t, dev, name)
     if t.dtype is not dtype:
         raise PagedError(f"{name} must be {dtype}, got {t.dtype}")
     got = t.shape
@@ -101,17 +120,17 @@ def _ptr(t, dtype, shape, name):
     return t.data_ptr()
 
 
-def _vec(t, dtype, n, name):
+def _vec(t, dtype, n, name, dev):
     """_ptr of a tensor with one axis, in fewer steps: the short calls' host time counts."""
-    if t.dtype is dtype and t.is_cuda and t.numel() == n and t.dim() == 1 and t.is_contiguous():
+    if t.dtype is dtype and t.get_device() == dev and t.numel() == n and t.dim() == 1 and t.is_contiguous():
         return t.data_ptr()
-    return _ptr(t, dtype, (n,), name)
+    return _ptr(t, dtype, (n,), name, dev)
 
 
-def _rows3(t, heads, dim, name):
+def _rows3(t, heads, dim, name, dev):
     """Address and strides of activations [rows, heads, dim] whose last axis is contiguous."""
-    if not t.is_cuda:
-        raise PagedError(f"{name} must be a device tensor")
+    if t.get_device() != dev:
+        raise _elsewhere(t, dev, name)
     if t.dtype not in ACTS:
         raise PagedError(f"{name} must be bfloat16 or float16, got {t.dtype}")
     if t.dim() != 3 or t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
@@ -127,9 +146,11 @@ def _rows3(t, heads, dim, name):
     return t.data_ptr(), row, head
 
 
-def _table(table, n=None):
+def _table(table, dev, n=None):
     """Address, stride and width of a block table [requests, width], its last axis contiguous."""
-    if not table.is_cuda or table.dtype is not torch.int32 or table.dim() != 2:
+    if table.get_device() != dev:
+        raise _elsewhere(table, dev, "table")
+    if table.dtype is not torch.int32 or table.dim() != 2:
         raise PagedError("table must be a device tensor of int32 [requests, width]")
     if n is not None and table.shape[0] != n:
         raise PagedError(f"table must have {n} rows, got {table.shape[0]}")
@@ -185,8 +206,8 @@ class PagedCache:
         for codes, scale, name in ((k, k_scale, "k"), (v, v_scale, "v")):
             if codes is None:
                 continue
-            if not codes.is_cuda or not scale.is_cuda:
-                raise PagedError(f"{name} and its scale must be device tensors")
+            if not codes.is_cuda or scale.get_device() != k.get_device() or codes.get_device() != k.get_device():
+                raise PagedError(f"{name} and its scale must be device tensors, on one device")
             if codes.dtype not in CODES:
                 raise PagedError(f"{name} must be float8_e4m3fn or int8, got {codes.dtype}")
             if codes.dim() != 4 or not codes[:1].is_contiguous():
@@ -205,6 +226,7 @@ class PagedCache:
                          self.n_heads if one else k_scale.stride(0),
                          self.n_pages, self.page, self.n_heads, self.head_dim, CODES[k.dtype])
         self._ref = ctypes.byref(self._c)
+        self._device = k.get_device()
         self._sizes = {}
         self.workspace, self._replaced = None, []
 
@@ -233,6 +255,12 @@ class PagedCache:
             ws[:WORKSPACE_ZEROED].zero_()
         return ws
 
+    def _on_current(self):
+        """The device of the cache, which has to be the current one (launches go there)."""
+        if self._device != _current_device():
+            raise PagedError(f"the cache is on cuda:{self._device}, but the current device is cuda:{_current_device()}")
+        return self._device
+
     def _space(self, workspace, n_rows, n_requests, heads, stream):
         need = self.workspace_size(n_rows, n_requests, heads)
         if workspace is None:
@@ -246,7 +274,9 @@ class PagedCache:
                     self._replaced.append(self.workspace)
                 self.workspace = made
             workspace = self.workspace
-        elif workspace.dtype is not torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
+        elif workspace.get_device() != self._device:
+            raise _elsewhere(workspace, self._device, "workspace")
+        elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
             raise PagedError("workspace must be a contiguous device tensor of uint8")
         return workspace.data_ptr(), workspace.numel()
 
@@ -259,56 +289,59 @@ def tables(ring, pool, lens, new_lens, table, page: int, *, pool_out, lens_out, 
     ``pool``; ``lens_out`` is another tensor than ``lens``."""
     n, rows = lens.numel(), slots.numel()
     i32 = torch.int32
-    at, stride, width = _table(table, n)
+    dev = _device(table, "table")
+    at, stride, width = _table(table, dev, n)
     _check((_lib or lib()).paged_kv_tables(
-        _ptr(ring, i32, (None,), "ring"), ring.numel(), _vec(pool, i32, 4, "pool"),
-        _vec(pool_out, i32, 4, "pool_out"), _vec(lens, i32, n, "lens"), _vec(new_lens, i32, n, "new_lens"),
-        _vec(lens_out, i32, n, "lens_out"), n, at, stride, width, page, rows,
-        _vec(row_starts, i32, n + 1, "row_starts"), _vec(row_request, i32, rows, "row_request"),
-        _vec(row_lengths, i32, rows, "row_lengths"), _vec(slots, torch.int64, rows, "slots"),
+        _ptr(ring, i32, (None,), "ring", dev), ring.numel(), _vec(pool, i32, 4, "pool", dev),
+        _vec(pool_out, i32, 4, "pool_out", dev), _vec(lens, i32, n, "lens", dev), _vec(new_lens, i32, n, "new_lens", dev),
+        _vec(lens_out, i32, n, "lens_out", dev), n, at, stride, width, page, rows,
+        _vec(row_starts, i32, n + 1, "row_starts", dev), _vec(row_request, i32, rows, "row_request", dev),
+        _vec(row_lengths, i32, rows, "row_lengths", dev), _vec(slots, torch.int64, rows, "slots", dev),
         _topk._stream(stream)), "paged_kv_tables")
 
 
 def store(cache: PagedCache, k_new, v_new, slots, stream=None) -> None:
     """Forwards to paged_kv_store(): new entries [rows, heads, dim] into the pages."""
-    k, k_row, k_head = _rows3(k_new, cache.n_heads, cache.head_dim, "k_new")
+    dev = cache._on_current()
+    k, k_row, k_head = _rows3(k_new, cache.n_heads, cache.head_dim, "k_new", dev)
     n = k_new.shape[0]
     v, v_row, v_head = None, 0, 0
     if v_new is not None:
-        v, v_row, v_head = _rows3(v_new, cache.n_heads, cache.head_dim, "v_new")
+        v, v_row, v_head = _rows3(v_new, cache.n_heads, cache.head_dim, "v_new", dev)
         if v_new.shape[0] != n or v_new.dtype is not k_new.dtype:
             raise PagedError("k_new and v_new must have one type and number of rows")
     if (v_new is None) != (cache.v is None):
         raise PagedError("v_new belongs to a cache with values, and to no other")
     _check((_lib or lib()).paged_kv_store(cache._ref, ACTS[k_new.dtype], k, k_row, k_head, v, v_row, v_head,
-                                          _vec(slots, torch.int64, n, "slots"), n, _topk._stream(stream)),
+                                          _vec(slots, torch.int64, n, "slots", dev), n, _topk._stream(stream)),
            "paged_kv_store")
 
 
-def _outputs(q, out, lse, stream):
+def _outputs(q, out, lse, stream, dev):
     if out is None and stream is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     elif out is None:  # of the stream that writes it: its memory may still be in use on the current one
         with _on(stream):
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    at = _ptr(out, q.dtype, q.shape, "out")
-    return out, at, _ptr(lse, torch.float32, q.shape[:2], "lse") if lse is not None else None
+    at = _ptr(out, q.dtype, q.shape, "out", dev)
+    return out, at, _ptr(lse, torch.float32, q.shape[:2], "lse", dev) if lse is not None else None
 
 
 def attend(cache: PagedCache, q, table, row_starts, row_lengths, scale: float, out=None, lse=None,
            workspace=None, stream=None):
     """Forwards to paged_kv_attend(): each row of q [rows, heads, dim] over the
     first row_lengths[i] tokens of its request.  Returns out."""
-    qp, q_row, q_head = _rows3(q, None, cache.head_dim, "q")
+    dev = cache._on_current()
+    qp, q_row, q_head = _rows3(q, None, cache.head_dim, "q", dev)
     rows, heads, _ = q.shape
-    at, stride, width = _table(table)
+    at, stride, width = _table(table, dev)
     n = table.shape[0]
-    out, op, lp = _outputs(q, out, lse, stream)
+    out, op, lp = _outputs(q, out, lse, stream, dev)
     ws, size = cache._space(workspace, rows, n, heads, stream)
     _check((_lib or lib()).paged_kv_attend(
         cache._ref, ACTS[q.dtype], qp, q_row, q_head, heads, at, stride, width,
-        _vec(row_starts, torch.int32, n + 1, "row_starts"), n,
-        _vec(row_lengths, torch.int32, rows, "row_lengths"), rows, scale, op, lp, ws, size,
+        _vec(row_starts, torch.int32, n + 1, "row_starts", dev), n,
+        _vec(row_lengths, torch.int32, rows, "row_lengths", dev), rows, scale, op, lp, ws, size,
         _topk._stream(stream)), "paged_kv_attend")
     return out
 
@@ -317,16 +350,17 @@ def attend_selected(cache: PagedCache, q, idx, table, row_request, row_lengths, 
                     workspace=None, stream=None):
     """Forwards to paged_kv_attend_selected(): each row of q over the tokens
     idx[i] of its request (a selection's out_idx).  Returns out."""
-    qp, q_row, q_head = _rows3(q, None, cache.head_dim, "q")
+    dev = cache._on_current()
+    qp, q_row, q_head = _rows3(q, None, cache.head_dim, "q", dev)
     rows, heads, _ = q.shape
-    at, stride, width = _table(table)
+    at, stride, width = _table(table, dev)
     n = table.shape[0]
-    out, op, lp = _outputs(q, out, lse, stream)
+    out, op, lp = _outputs(q, out, lse, stream, dev)
     ws, size = cache._space(workspace, rows, n, heads, stream)
     _check((_lib or lib()).paged_kv_attend_selected(
-        cache._ref, ACTS[q.dtype], qp, q_row, q_head, heads, _ptr(idx, torch.int32, (rows, None), "idx"),
-        idx.shape[1], at, stride, width, _vec(row_request, torch.int32, rows, "row_request"), n,
-        _vec(row_lengths, torch.int32, rows, "row_lengths"), rows, scale, op, lp, ws, size,
+        cache._ref, ACTS[q.dtype], qp, q_row, q_head, heads, _ptr(idx, torch.int32, (rows, None), "idx", dev),
+        idx.shape[1], at, stride, width, _vec(row_request, torch.int32, rows, "row_request", dev), n,
+        _vec(row_lengths, torch.int32, rows, "row_lengths", dev), rows, scale, op, lp, ws, size,
         _topk._stream(stream)), "paged_kv_attend_selected")
     return out
 
@@ -335,12 +369,13 @@ def score(cache: PagedCache, q, w, table, row_request, row_lengths, scale: float
           stream=None) -> None:
     """Forwards to paged_kv_score(): row i's scores of its visible tokens to
     scores[row_offsets[i] ..] (any contiguous float32 tensor), as topk_ragged reads them."""
-    qp, q_row, q_head = _rows3(q, None, cache.head_dim, "q")
+    dev = cache._on_current()
+    qp, q_row, q_head = _rows3(q, None, cache.head_dim, "q", dev)
     rows, heads, _ = q.shape
-    at, stride, width = _table(table)
+    at, stride, width = _table(table, dev)
     _check((_lib or lib()).paged_kv_score(
-        cache._ref, ACTS[q.dtype], qp, q_row, q_head, heads, _ptr(w, torch.float32, (rows, heads), "w"), at, stride,
-        width, _vec(row_request, torch.int32, rows, "row_request"), table.shape[0],
-        _vec(row_lengths, torch.int32, rows, "row_lengths"), rows, scale,
-        _ptr(scores, torch.float32, scores.shape, "scores"), _vec(row_offsets, torch.int64, rows, "row_offsets"),
+        cache._ref, ACTS[q.dtype], qp, q_row, q_head, heads, _ptr(w, torch.float32, (rows, heads), "w", dev), at, stride,
+        width, _vec(row_request, torch.int32, rows, "row_request", dev), table.shape[0],
+        _vec(row_lengths, torch.int32, rows, "row_lengths", dev), rows, scale,
+        _ptr(scores, torch.float32, scores.shape, "scores", dev), _vec(row_offsets, torch.int64, rows, "row_offsets", dev),
         _topk._stream(stream)), "paged_kv_score")
