@@ -132,7 +132,10 @@ size_t paged_kv_attend_workspace(int32_t n_rows, int32_t n_requests, int32_t hea
  *   table   int32 [n_requests][table_stride], table_width entries used;
  *   heads   a multiple of the cache's n_heads;
  *   scale   finite and not negative.
- * A row that sees no token, or that no request has, gets 0 and -inf. */
+ * A row that sees no token, or that no request has (row_starts[0] may be past 0), gets
+ * 0 and -inf.  Scores, sums and lse are FP32; weights are rounded to f16 before they
+ * meet the values, whatever q's type: 11 bits down to 2^-20 of the row's largest
+ * product of weight and value scale. */
 int paged_kv_attend(const paged_kv_cache *cache, int32_t act, const void *q, int64_t q_row,
                     int64_t q_head, int32_t heads, const int32_t *table, int32_t table_stride,
                     int32_t table_width, const int32_t *row_starts, int32_t n_requests,

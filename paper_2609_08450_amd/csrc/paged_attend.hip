@@ -128,7 +128,9 @@ Shape shape_of(int n_rows, int n_requests, int heads, int kv_heads, int dim, boo
     }
     // up to three rows to a request each row reads the cache by itself (64 rows of 32
     // requests at 16384 to 32768 tokens: 127 us, and 227 as a
-    // prompt; three to a request: 180 and 230)
+    // prompt; three to a request: 180 and 230).  One rule for the call, in which
+    // n_requests is the table's height: a prompt among many single rows, or in a table
+    // of many idle requests, is read row by row.
     s.prompt = n_rows > 3 * (int64_t)n_requests;
     if (s.prompt) {
         s.cols = dim == 256 ? 128 : 256;

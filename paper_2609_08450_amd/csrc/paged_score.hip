@@ -11,9 +11,10 @@
 //     multiply-add), and by the 4 bytes written for each;
 //   single rows (score_row_kernel): bound by the keys' D bytes a token; every
 //     wave streams tokens of its own.
-// Measured (8 heads of 64): 4096 rows over 131072 tokens 632 us, 860 TFLOP/s beside
-// 3.4 TB/s of writes, at the card's power limit; 64 rows of 16384 to 131072 tokens
-// 66.6 us, 4.6 TB/s.
+// Measured (8 heads of 64): 4096 rows over 131072 tokens 620 us, 873 TFLOP/s beside
+// 3.4 TB/s of writes, at a clock of 1.91 GHz (a large matrix product runs at 1.94 and
+// reaches 1415, calls that memory bounds run at 2.40); 64 rows of 16384 to 131072
+// tokens 66.7 us, 4.6 TB/s.
 #include "paged_common.h"
 #include "paged_score_plan.h"
 
@@ -379,7 +380,11 @@ extern "C" int paged_kv_score(const paged_kv_cache *cache, int32_t act, const vo
     int tokens = kBlock / 64 * 32 * tokens_of(cache->head_dim, heads > 2 ? 4 : 1);  // of a workgroup's step
     if (n_rows > n_requests || n_rows > 65535) {
         // rows share their keys: as many to a workgroup as its LDS holds, and so
-        // many workgroups to a window as give the card 1024 (2 to a CU are resident)
+        // many workgroups to a window as give the card 1024 (2 to a CU are resident).
+        // One rule for the call, in which n_requests is the table's height: rows of one
+        // request gain from windows (16 over 131072 tokens 9.3 us, and 21.4 by themselves;
+        // eight of each of 64 requests of 16384 46 and 73), but few rows of many requests
+        // lose (two of each of the 64: 131 us, and 25 by themselves; four: 66 and 41).
         a.window = rows_of_window(cache->head_dim, heads);
         const int64_t windows = ((int64_t)n_rows + a.window - 1) / a.window;
         const int64_t blocks = (cap + tokens - 1) / tokens, want = (1024 + windows - 1) / windows;

@@ -3,9 +3,10 @@
 // A run is the rows of one page (they follow each other, at consecutive places).
 // One wave takes a run of one head and side at a time: its rows into registers,
 // their largest magnitude, the page's scale, then the codes; no wave waits for
-// another.  Bound by memory where the rows are many (3 bytes an element), by the
-// chain slots - rows - codes where they are few.  8192 rows of 8 heads of 128, K and
-// V, int8: 15.5 us, 3.2 TB/s; 64 single rows: 7.3 us.
+// another.  Bound by memory (3 bytes an element) and by vector work (24 instructions
+// an element, 10 us of a SIMD's time in the first case below) where the rows are
+// many, by the chain slots - rows - codes where they are few.  8192 rows of 8 heads
+// of 128, K and V, int8: 15.7 us, 3.2 TB/s; 64 single rows: 7.6 us.
 #include "paged_common.h"
 
 namespace paged {

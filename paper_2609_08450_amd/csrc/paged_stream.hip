@@ -14,9 +14,12 @@
 // weighted with V's scale over a reference of each column's own that follows the
 // largest product of weight and scale seen so far: full bits down to 2^-20 of that
 // product, whatever the scales of pages that weigh nothing.
-// Measured (heads of 128, e4m3): 64 rows of 16384 to 131072 tokens 396 us, 5.83
-// TB/s; one row of 131071 tokens on 8 heads 57 us; 4096 rows of 2048 selected
-// tokens 266 us, 8.1 TB/s of gathers out of the last-level cache.
+// (Of the scale alone instead, a page with values 2^22 times as large took the others'
+// bits and 2^30 times the others, where it weighed nothing: one long row took 59.2 us
+// instead of 60.7 then, the selected prompt block 255 instead of 258.)
+// Measured (heads of 128, e4m3): 64 rows of 16384 to 131072 tokens 402 us, 5.75
+// TB/s; one row of 131071 tokens on 8 heads 58.3 us; 4096 rows of 2048 selected
+// tokens 268 us, 8.0 TB/s of gathers beside vector work in half of the cycles.
 #include "paged_attend.h"
 
 namespace paged {
