@@ -35,3 +35,17 @@ def test_an_output_that_a_call_makes_belongs_to_its_stream(selected):
         assert out.data_ptr() != where
         torch.cuda.synchronize()
         assert_attention(out, None, ref, "output of another stream")
+
+
+def test_the_default_streams_handle():
+    """A program may hand over the number of the stream that is current, 0 for the default one."""
+    from paper_2609_08450_amd import paged
+
+    s = Setup([700, 300], [1, 1], page=32, kv=2, heads=8, dim=128).cuda()
+    ref, cache = attention(s), s.cache()
+    assert torch.cuda.current_stream().cuda_stream == 0
+    for _ in range(2):  # with the workspace's first call, and after it
+        out = paged.attend(cache, s.q, s.table, s.row_starts, s.row_lengths, s.scale, stream=0)
+        torch.cuda.synchronize()
+        assert_attention(out, None, ref, "stream 0")
+    assert torch.cuda.current_stream().cuda_stream == 0
