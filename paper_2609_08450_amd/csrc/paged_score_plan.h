@@ -26,11 +26,12 @@ constexpr int rows_of_window(int dim, int heads) {
     return window_of(dim) / (32 * product_chunks(heads)) * (32 / product_heads(heads));
 }
 
+// (A window of one row stands for the kernel of single rows.)
 constexpr bool windows_fit() {
     for (int dim = 64; dim <= 128; dim += 64)
         for (int heads = 1; heads <= 128; ++heads) {
             const int rows = rows_of_window(dim, heads);
-            if (rows < 1 || 32 * products_of(rows, heads) > window_of(dim)) return false;
+            if (rows < 2 || 32 * products_of(rows, heads) > window_of(dim)) return false;
         }
     return true;
 }

@@ -67,6 +67,13 @@ def test_head_layouts(heads, kv):
         check(Setup(lens, [9, 2, 1], heads=heads, kv=kv, dim=128, act=act, page=32), where="heads of a prompt")
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_more_heads_than_a_group_has_columns(dim):
+    """A row's heads on one cache head are cut into parts, the last one not full."""
+    for lens, rows in (([700, 33], [1, 1]), ([700, 33], [9, 2]), ([20000], [5])):
+        check(Setup(lens, rows, heads=300, kv=1, dim=dim, page=32), where="many heads")
+
+
 @pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
 def test_one_long_row(page):
     """One row over the whole card: many workgroups join their parts."""
