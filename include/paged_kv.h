@@ -156,7 +156,8 @@ int paged_kv_attend_selected(const paged_kv_cache *cache, int32_t act, const voi
  * for j < row_lengths[i], over the keys of a cache with one head: the rows that
  * topk_ragged selects from.  Nothing past a row's length is written; at the
  * tokens of a page outside the cache the score is -inf.
- *   q    as above, `heads` from 1 to 128;  w  FP32 [n_rows][heads];
+ *   q    as above, `heads` from 1 to 128;  w  FP32 [n_rows][heads]; both finite
+ *        (a product that is NaN may count as 0);
  *   row_offsets  int64 [n_rows], in elements. */
 int paged_kv_score(const paged_kv_cache *cache, int32_t act, const void *q, int64_t q_row,
                    int64_t q_head, int32_t heads, const float *w, const int32_t *table,
