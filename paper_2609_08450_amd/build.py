@@ -1,5 +1,6 @@
 """Builds the HIP libraries in-tree for gfx950 with hipcc: libtopk_ragged.so
-(the selection) and libpaged_kv.so (the paged 8-bit cache around it)."""
+(the selection), libpaged_kv.so (the paged 8-bit cache around it) and
+libserve_step.so (positions, eviction and logits on either side)."""
 from __future__ import annotations
 
 import os
@@ -13,6 +14,8 @@ LIB_PATH = os.path.join(HERE, "libtopk_ragged.so")
 PAGED_SRCS = [os.path.join(HERE, "csrc", f"paged_{name}.hip")
               for name in ("tables", "store", "attend", "stream", "prompt", "score")]
 PAGED_LIB_PATH = os.path.join(HERE, "libpaged_kv.so")
+SERVE_SRCS = [os.path.join(HERE, "csrc", f"serve_{name}.hip") for name in ("rotate", "weigh", "evict", "logits")]
+SERVE_LIB_PATH = os.path.join(HERE, "libserve_step.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc" if os.path.exists("/opt/rocm/bin/hipcc")
                        else (shutil.which("hipcc") or "hipcc"))
 
@@ -53,10 +56,11 @@ def _end(proc: subprocess.Popen, verbose: bool) -> None:
         print("\n".join(msgs))
 
 
-def build_paged(verbose: bool = False) -> str:
+def _build_of(srcs: list[str], path: str, verbose: bool) -> str:
+    """A library of several sources, each compiled by itself."""
     with tempfile.TemporaryDirectory() as tmp:
-        objs = [os.path.join(tmp, os.path.basename(s) + ".o") for s in PAGED_SRCS]
-        procs = [_run([HIPCC, *BASE_FLAGS, "-c", s, "-o", o], verbose) for s, o in zip(PAGED_SRCS, objs)]
+        objs = [os.path.join(tmp, os.path.basename(s) + ".o") for s in srcs]
+        procs = [_run([HIPCC, *BASE_FLAGS, "-c", s, "-o", o], verbose) for s, o in zip(srcs, objs)]
         try:
             for p in procs:
                 _end(p, verbose)
@@ -64,15 +68,24 @@ def build_paged(verbose: bool = False) -> str:
             for p in procs:
                 if p.poll() is None:
                     p.kill()
-        _end(_run([HIPCC, "--offload-arch=gfx950", "-shared", "-o", PAGED_LIB_PATH + ".tmp", *objs], verbose), verbose)
-    os.replace(PAGED_LIB_PATH + ".tmp", PAGED_LIB_PATH)
-    return PAGED_LIB_PATH
+        _end(_run([HIPCC, "--offload-arch=gfx950", "-shared", "-o", path + ".tmp", *objs], verbose), verbose)
+    os.replace(path + ".tmp", path)
+    return path
+
+
+def build_paged(verbose: bool = False) -> str:
+    return _build_of(PAGED_SRCS, PAGED_LIB_PATH, verbose)
+
+
+def build_serve(verbose: bool = False) -> str:
+    return _build_of(SERVE_SRCS, SERVE_LIB_PATH, verbose)
 
 
 def build(verbose: bool = False) -> str:
     topk = _run([HIPCC, *FLAGS, "-o", LIB_PATH + ".tmp", SRC], verbose)
     try:
         build_paged(verbose)
+        build_serve(verbose)
     finally:
         _end(topk, verbose)
     os.replace(LIB_PATH + ".tmp", LIB_PATH)

@@ -7,7 +7,7 @@
 // an element, 10 us of a SIMD's time in the first case below) where the rows are
 // many, by the chain slots - rows - codes where they are few.  8192 rows of 8 heads
 // of 128, K and V, int8: 15.7 us, 3.2 TB/s; 64 single rows: 7.6 us.
-#include "paged_common.h"
+#include "paged_codes.h"
 
 namespace paged {
 namespace {
@@ -30,20 +30,6 @@ struct StoreArgs {
     int64_t page_stride, scale_stride;
     int n_rows, lp, dim, splits;
 };
-
-constexpr float kLeast = 7.888609052210118e-31f;  // 2^-100
-
-template <class C>
-__device__ float scale_of(float top);
-template <>
-__device__ float scale_of<E4M3>(float top) {
-    // least power of two s with 448 s >= top; 448 = 1.75 * 2^8
-    const u32 b = __float_as_uint(top);
-    const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-    return __uint_as_float((u32)(max(e, -100) + 127) << 23);
-}
-template <>
-__device__ float scale_of<Int8>(float top) { return fmaxf(__fmul_rn(top, 1.0f / 127.0f), kLeast); }
 
 // Codes of x / s, eight at a time, x finite or not.
 template <class C>
@@ -100,13 +86,6 @@ __device__ u32x2 codes_of<Int8>(const float (&x)[8], float s) {
     }
     return z;
 }
-
-template <class C>
-__device__ float value_of(u32 code);
-template <>
-__device__ float value_of<E4M3>(u32 code) { return __builtin_amdgcn_cvt_f32_fp8((int)code, 0); }
-template <>
-__device__ float value_of<Int8>(u32 code) { return (float)(signed char)code; }
 
 template <class T>
 __device__ void elements(u32x4 v, float (&x)[8]) {
