@@ -18,6 +18,7 @@ namespace {
 
 constexpr int kKeep = 1024;
 constexpr int kWords = 16384;  // words of LDS: 2^19 tokens at a time
+constexpr int kList = 4096;    // kept tokens that are written at a time
 
 struct KeepArgs {
     const int *idx;
@@ -60,11 +61,13 @@ __device__ u32 bits_of(int64_t at, int64_t from, int64_t to) {
 
 __global__ __launch_bounds__(kKeep) void keep_kernel(KeepArgs a) {
     __shared__ u32 words[kWords];
+    __shared__ int list[kList];
     __shared__ int waves[kKeep / 64];
     const int tid = threadIdx.x, r = blockIdx.x;
     const int len = max(a.lens[r], 0);
     const int *idx = a.idx + (int64_t)r * a.K;
     int *kept = a.kept + (int64_t)r * a.width;
+    float *weights = a.weights ? a.weights + a.weight_offsets[r] : nullptr;
     int count = 0;
     for (int64_t base = 0; base < len; base += 32 * (int64_t)kWords) {
         const int tokens = (int)min((int64_t)len - base, 32 * (int64_t)kWords), n = (tokens + 31) / 32;
@@ -82,32 +85,37 @@ __global__ __launch_bounds__(kKeep) void keep_kernel(KeepArgs a) {
         const int per = (n + kKeep - 1) / kKeep, from = min(tid * per, n), to = min(from + per, n);
         int mine = 0, all;
         for (int i = from; i < to; ++i) mine += __popc(words[i]);
-        int at = count + prefix(mine, waves, &all);
-        for (int i = from; i < to; ++i)
-            for (u32 w = words[i]; w; w &= w - 1) kept[at++] = (int)(base + 32 * i + __builtin_ctz(w));
+        const int at = count + prefix(mine, waves, &all);
+        // in order, by way of LDS
+        for (int done = 0; done < all; done += kList) {
+            int to_place = at - count - done;
+            for (int i = from; i < to && to_place < kList; ++i)
+                for (u32 w = words[i]; w; w &= w - 1, ++to_place)
+                    if (to_place >= 0 && to_place < kList) list[to_place] = (int)(base + 32 * i + __builtin_ctz(w));
+            __syncthreads();
+            const int n = min(all - done, kList);
+            float x[kList / kKeep];
+#pragma unroll
+            for (int j = 0; j < kList / kKeep; ++j) {
+                const int i = j * kKeep + tid;
+                if (i >= n) continue;
+                kept[count + done + i] = list[i];
+                if (weights) x[j] = weights[list[i]];
+            }
+            __syncthreads();
+            if (weights)
+#pragma unroll
+                for (int j = 0; j < kList / kKeep; ++j) {
+                    const int i = j * kKeep + tid;
+                    if (i < n) weights[count + done + i] = x[j];
+                }
+        }
         count += all;
-        __syncthreads();
     }
     for (int i = count + tid; i < a.width; i += kKeep) kept[i] = -1;
     if (tid == 0) a.counts[r] = count;
-    if (!a.weights) return;
-    float *w = a.weights + a.weight_offsets[r];
-    for (int i0 = 0; i0 < count; i0 += 4 * kKeep) {
-        float x[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int i = i0 + j * kKeep + tid;
-            if (i < count) x[j] = w[kept[i]];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int i = i0 + j * kKeep + tid;
-            if (i < count) w[i] = x[j];
-        }
-        __syncthreads();
-    }
-    for (int64_t i = (int64_t)count + tid; i < len; i += kKeep) w[i] = 0.0f;
+    if (weights)
+        for (int64_t i = (int64_t)count + tid; i < len; i += kKeep) weights[i] = 0.0f;
 }
 
 struct CompactArgs {
@@ -123,7 +131,6 @@ struct CompactArgs {
     const int *counts;
 };
 
-constexpr int kPart = 8192;  // bytes of codes that a wave holds
 constexpr u32 kNone = 0xFFFFFFFFu;
 
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
@@ -157,91 +164,97 @@ __device__ inline float largest<Int8>(u32x4 x) {
     return (float)(max(max((int)hi[0], (int)hi[1]), -min((int)lo[0], (int)lo[1])) >> 8);
 }
 
-// Codes of (code * old) / s, 16 at a time; ratio is old / s.
+// Codes of (code * old) / s, 16 at a time; no quotient is past the type's largest.
 template <class C>
-__device__ u32x4 anew(u32x4 x, float old, float s, float ratio);
+__device__ u32x4 anew(u32x4 x, float old, float s);
 template <>
-__device__ inline u32x4 anew<E4M3>(u32x4 x, float old, float s, float) {
-    // the product with a power of two is exact: one rounding to FP32, one to a code
-    const float r = __uint_as_float((254u << 23) - __float_as_uint(s));
+__device__ inline u32x4 anew<E4M3>(u32x4 x, float old, float s) {
+    // s is a power of two, so that the factor is exact, and the product with it rounds as the
+    // one with `old` does: once to FP32, once to a code.  (A factor this large is one of codes 0.)
+    const float by = fminf(old * __uint_as_float((254u << 23) - __float_as_uint(s)), 1e30f);
     u32x4 z;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        float y[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            y[i] = __fmul_rn(value_of<E4M3>((x[j] >> (8 * i)) & 0xFFu), old);
-            y[i] = __builtin_amdgcn_fmed3f(y[i] * r, -448.0f, 448.0f);
-        }
-        const int c = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-        z[j] = (u32)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], c, true);
+        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)x[j], false);
+        const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)x[j], true);
+        const int c = __builtin_amdgcn_cvt_pk_fp8_f32(lo[0] * by, lo[1] * by, 0, false);
+        z[j] = (u32)__builtin_amdgcn_cvt_pk_fp8_f32(hi[0] * by, hi[1] * by, c, true);
     }
     return z;
 }
 template <>
-__device__ inline u32x4 anew<Int8>(u32x4 x, float old, float s, float ratio) {
-    // The product with the rounded ratio is within 128 * 2^-23 of the quotient, so it
-    // rounds to the same unless it lies that near a half: then the wave divides, in 64
-    // bits.  Added to 1.5 * 2^23 a product has its whole number in the lowest byte.
+__device__ inline u32x4 anew<Int8>(u32x4 x, float old, float s) {
+    // The product with the rounded ratio is within 1.2e-5 of the quotient (2^-24 of 127, and half a
+    // step at 127), so it rounds to the same unless it lies that near a half.  Added to
+    // 1.5 * 2^23 a product has its whole number in the lowest byte.  (Codes as unsigned
+    // bytes, 128 too large, take one instruction to convert.)
     constexpr float kWhole = 12582912.0f;
+    const float ratio = fminf(__fdiv_rn(old, s), 1e30f), less = -128.0f * ratio;  // (this large: codes are 0)
     u32x4 z;
     float off = 0.0f;
+    const auto packed = [](const u32 (&y)[4]) {
+        return __builtin_amdgcn_perm(y[1], y[0], 0x0c0c0400u) | __builtin_amdgcn_perm(y[3], y[2], 0x04000c0cu);
+    };
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
+        const u32 u = x[j] ^ 0x80808080u;
         u32 y[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float q = __builtin_amdgcn_fmed3f(value_of<Int8>((x[j] >> (8 * i)) & 0xFFu) * ratio, -127.0f, 127.0f);
+            const float q = fmaf((float)((u >> (8 * i)) & 0xFFu), ratio, less);
             const float n = q + kWhole;
             y[i] = __float_as_uint(n);
             off = fmaxf(off, fabsf(q - (n - kWhole)));
         }
-        const u32 lo = __builtin_amdgcn_perm(y[1], y[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(y[3], y[2], 0x04000c0cu);
-        z[j] = lo | hi;
+        z[j] = packed(y);
     }
-    if (!(off < 0.4999f)) {
-        u32 w[4] = {x[0], x[1], x[2], x[3]};
+    if (!(off < 0.49998f)) {
+        // code * old against h * s, h the half next to the product: its rounded product with s
+        // taken from both, what is left of either is exact
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            u32 all = 0;
-#pragma unroll 1
-            for (int i = 0; i < 32; i += 8) {
-                const double q = rint((double)(signed char)(w[j] >> i) * (double)old / (double)s);
-                all |= ((u32)(int)fmin(fmax(q, -127.0), 127.0) & 0xFFu) << i;
+            u32 y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float c = value_of<Int8>((x[j] >> (8 * i)) & 0xFFu);
+                const float below = floorf(c * ratio), h = below + 0.5f, p = h * s;
+                const float d = fmaf(c, old, -p) - fmaf(h, s, -p);
+                const bool odd = (int)below & 1;
+                y[i] = __float_as_uint(below + (d > 0.0f || (d == 0.0f && odd) ? 1.0f : 0.0f) + kWhole);
             }
-            z[j] = all;
+            z[j] = packed(y);
         }
     }
     return z;
 }
 
-// The maxima of eight values over the wave: that of value i in the lanes l with l / 8 == i.
-__device__ inline float eight_tops(const float (&t)[8]) {
+// The maxima of N values over the wave: that of value i in the lanes l with l / (64 / N) == i.
+template <int N>
+__device__ float tops_of(float (&t)[N]) {
     const int lane = threadIdx.x & 63;
-    float u[4], v[2];
+    int d = 32;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float keep = lane & 32 ? t[i + 4] : t[i], send = lane & 32 ? t[i] : t[i + 4];
-        u[i] = fmaxf(keep, __shfl_xor(send, 32));
-    }
+    for (int n = N / 2; n; n /= 2, d /= 2)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const float keep = lane & 16 ? u[i + 2] : u[i], send = lane & 16 ? u[i] : u[i + 2];
-        v[i] = fmaxf(keep, __shfl_xor(send, 16));
-    }
-    const float keep = lane & 8 ? v[1] : v[0], send = lane & 8 ? v[0] : v[1];
-    float w = fmaxf(keep, __shfl_xor(send, 8));
-#pragma unroll
-    for (int d = 4; d; d >>= 1) w = fmaxf(w, __shfl_xor(w, d));
-    return w;
+        for (int i = 0; i < n; ++i) {
+            const float keep = lane & d ? t[i + n] : t[i], send = lane & d ? t[i] : t[i + n];
+            t[i] = fmaxf(keep, __shfl_xor(send, d));
+        }
+    for (; d; d /= 2) t[0] = fmaxf(t[0], __shfl_xor(t[0], d));
+    return t[0];
 }
 
-template <class C, int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void compact_kernel(CompactArgs a) {
-    constexpr int TOKENS = kPart / D;     // of a wave's part
+// All waves are here, and what they wrote to LDS.  (Not __syncthreads(): that would wait for the
+// loads that are on their way, too.)
+__device__ inline void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// WAVES of a workgroup hold PIECES of 1024 bytes of codes each, at least a page of 64 KB together.
+template <class C, int D, int WAVES, int PIECES>
+__global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
+    constexpr int TOKENS = PIECES * 1024 / D;  // of a wave's part
     constexpr int SLOTS = (TOKENS + 63) / 64;
-    constexpr int PIECES = kPart / 1024;  // of 16 bytes, of a lane
     __shared__ float tops[2][PIECES * WAVES];
+    __shared__ int first_moved;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int r = blockIdx.y, head = blockIdx.x / a.sides;
     uint8_t *codes = a.codes[blockIdx.x % a.sides];
@@ -251,64 +264,108 @@ __global__ __launch_bounds__(64 * WAVES) void compact_kernel(CompactArgs a) {
     const int count = (int)min((int64_t)min(max(a.counts[r], 0), a.width), cap);
     const int *table = a.table + (int64_t)r * a.table_stride;
     const int *kept = a.kept + (int64_t)r * a.width;
-    const auto page_of = [&](int i) {
-        const int p = table[i];
-        return p >= 0 && p < a.n_pages ? p : -1;
-    };
 
-    // the first page that changes: kept rises, so whole pages before a token that moves
-    // stay if their last token does
-    int stay = 0;
-    {
-        int lo = 0, hi = count;  // kept[i] == i for i < lo
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (kept[mid] == mid) lo = mid + 1;
-            else hi = mid;
+    // the first page that changes: kept rises, so a page stays if its last token does
+    const int pages = (count + P - 1) >> a.lp;
+    int stay = pages;
+    for (int p = tid; p < pages; p += 64 * WAVES) {
+        const int last = min((int)min(((int64_t)p + 1) << a.lp, (int64_t)0x7FFFFFFF), count) - 1;
+        if (kept[last] != last) {
+            stay = p;
+            break;
         }
-        if (lo == count) return;
-        stay = lo >> a.lp;
     }
-    // a round: TOKENS of each wave, from a multiple of the page's on
-    const int round = TOKENS * WAVES;
-    int turn = 0;
-    for (int64_t base = (int64_t)stay << a.lp; base < count; base += round, turn ^= 1) {
-        const int64_t mine = base + (int64_t)wave * TOKENS;
-        // this lane's tokens: the row of codes that each comes from, its scale
-        u32 from[SLOTS];
-        float old[SLOTS];
+    if (tid == 0) first_moved = pages;
+    __syncthreads();
+    if (stay < pages) atomicMin(&first_moved, stay);
+    __syncthreads();
+    stay = first_moved;
+    if (stay == pages) return;
+
+    // A round: TOKENS of each wave.  Four of them are on their way at a time: the numbers of
+    // kept tokens, pages, scales and codes each need those before.
+    const int64_t begin = ((int64_t)stay << a.lp) + (int64_t)wave * TOKENS;
+    constexpr int64_t ROUND = TOKENS * WAVES;
+    const u32 head_row = (u32)(head << a.lp);
+    int kk[SLOTS], pg[SLOTS], pk[SLOTS];  // kept tokens, and pages with the tokens that they are of
+    u32 from[SLOTS];
+    float old[SLOTS], next_old[SLOTS];
+    int to, next_to;  // lane i: the page that piece i goes to
+    const auto numbers = [&](int64_t at) {
 #pragma unroll
         for (int i = 0; i < SLOTS; ++i) {
-            const int64_t t = mine + 64 * i + lane;
+            const int64_t t = at + 64 * i + lane;
+            kk[i] = -1;
+            if (lane < TOKENS && t < count) kk[i] = kept[t];
+        }
+    };
+    const auto target = [&](int64_t at) {
+        const int64_t t = at + lane * (1024 / D);
+        next_to = -1;
+        if (lane < PIECES && t < count) next_to = table[t >> a.lp];
+    };
+    const auto look_up = [&] {
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) {
+            pk[i] = kk[i];
+            pg[i] = -1;
+            if (kk[i] >= 0 && kk[i] < cap) pg[i] = table[kk[i] >> a.lp];
+        }
+    };
+    const auto rows = [&] {
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) {
             from[i] = kNone;
-            old[i] = 0.0f;
-            if (lane < TOKENS && t < count) {
-                const int k = kept[t];
-                if (k < 0 || k >= cap) continue;
-                const int p = page_of(k >> a.lp);
-                if (p < 0) continue;
-                from[i] = (u32)p * a.page_rows + (u32)(head << a.lp) + (u32)(k & (P - 1));
-                old[i] = scales[p * a.scale_stride];
+            next_old[i] = 0.0f;
+            if (pg[i] >= 0 && pg[i] < a.n_pages) {
+                from[i] = (u32)pg[i] * a.page_rows + head_row + (u32)(pk[i] & (P - 1));
+                next_old[i] = scales[pg[i] * a.scale_stride];
             }
         }
-        u32x4 x[PIECES];
-        float scale[PIECES];
+    };
+    const auto fetch = [&](u32x4 (&x)[PIECES]) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int t = (1024 * i + 16 * lane) / D;  // token of the part
             const u32 row = __shfl(from[SLOTS == 1 ? 0 : t >> 6], t & 63);
-            scale[i] = __shfl(old[SLOTS == 1 ? 0 : t >> 6], t & 63);
             x[i] = u32x4{0, 0, 0, 0};
             if (row != kNone) x[i] = *(const u32x4 *)(codes + (int64_t)row * D + (16 * lane) % D);
         }
+    };
+    u32x4 x[PIECES], next[PIECES];
+    numbers(begin);
+    look_up();
+    numbers(begin + ROUND);
+    rows();
+    look_up();
+    numbers(begin + 2 * ROUND);
+    target(begin);
+    fetch(next);
+    int turn = 0;
+    for (int64_t mine = begin; mine - (int64_t)wave * TOKENS < count; mine += ROUND, turn ^= 1) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) x[i] = next[i];
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) old[i] = next_old[i];
+        to = next_to;
+        rows();
+        look_up();
+        numbers(mine + 3 * ROUND);
+        target(mine + ROUND);
+        fetch(next);
+
         // the largest magnitude of every 1024 bytes
+        const auto scale_at = [&](int i) {
+            const int t = (1024 * i + 16 * lane) / D;
+            return __shfl(old[SLOTS == 1 ? 0 : t >> 6], t & 63);
+        };
         float top[PIECES];
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) top[i] = __fmul_rn(largest<C>(x[i]), scale[i]);
-        const float mine_top = eight_tops(top);
-        if (lane % 8 == 0) tops[turn][wave * PIECES + lane / 8] = mine_top;
+        for (int i = 0; i < PIECES; ++i) top[i] = __fmul_rn(largest<C>(x[i]), scale_at(i));
+        const float mine_top = tops_of(top);
+        if (lane % (64 / PIECES) == 0) tops[turn][wave * PIECES + lane / (64 / PIECES)] = mine_top;
         // all of this round is read, and its maxima are there
-        __syncthreads();
+        meet();
         const int group = (D << a.lp) / 1024;  // entries of `tops` to a page
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
@@ -316,22 +373,30 @@ __global__ __launch_bounds__(64 * WAVES) void compact_kernel(CompactArgs a) {
             float m = 0.0f;
             for (int j = 0; j < group; ++j) m = fmaxf(m, tops[turn][at + j]);
             const float s = scale_of<C>(m);
-            const int64_t t = mine + (1024 * i + 16 * lane) / D;
-            const int page = t < count ? page_of((int)(t >> a.lp)) : -1;
-            if (page < 0) continue;
-            const float ratio = __fdiv_rn(scale[i], s);
-            const u32x4 y = anew<C>(x[i], scale[i], s, ratio);
-            const u32 row = (u32)page * a.page_rows + (u32)(head << a.lp) + (u32)(t & (P - 1));
-            *(u32x4 *)(codes + (int64_t)row * D + (16 * lane) % D) = y;
-            if ((t & (P - 1)) == 0 && (16 * lane) % D == 0) scales[page * a.scale_stride] = s;
+            __builtin_amdgcn_sched_barrier(0);  // one after the other: registers
+            // a piece lies in one page
+            const int page = __builtin_amdgcn_readlane(to, i);
+            const int64_t t = mine + 1024 * i / D;
+            if (page < 0 || page >= a.n_pages) continue;
+            // (codes under the scale that the page gets are what they are)
+            const float was = scale_at(i);
+            const u32x4 y = was == s ? x[i] : anew<C>(x[i], was, s);
+            const u32 row = (u32)page * a.page_rows + head_row + (u32)(t & (P - 1));
+            if (t + 16 * lane / D < count) *(u32x4 *)(codes + (int64_t)row * D + 16 * lane) = y;
+            if ((t & (P - 1)) == 0 && lane == 0) scales[page * a.scale_stride] = s;
         }
     }
 }
 
+#ifndef KW
+#define KW 16
+#endif
+constexpr int kWaves = KW, kPieces = 64 / KW;
+
 template <class C, int D>
 int launch_compact(const CompactArgs &a, int n_requests, void *stream) {
     const dim3 grid((unsigned)(a.n_heads * a.sides), (unsigned)n_requests);
-    return launch(compact_kernel<C, D, 8>, grid, dim3(512), stream, a);
+    return launch(compact_kernel<C, D, kWaves, kPieces>, grid, dim3(64 * kWaves), stream, a);
 }
 
 }  // namespace
