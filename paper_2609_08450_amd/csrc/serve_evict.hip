@@ -187,7 +187,7 @@ __device__ inline u32x4 anew<Int8>(u32x4 x, float old, float s) {
     // The product with the rounded ratio is within 1.2e-5 of the quotient (2^-24 of 127, and half a
     // step at 127), so it rounds to the same unless it lies that near a half.  Added to
     // 1.5 * 2^23 a product has its whole number in the lowest byte.  (Codes as unsigned
-    // bytes, 128 too large, take one instruction to convert.)
+    // bytes, 128 too large, take one instruction to convert; 128 ratios less is exact.)
     constexpr float kWhole = 12582912.0f;
     const float ratio = fminf(__fdiv_rn(old, s), 1e30f), less = -128.0f * ratio;  // (this large: codes are 0)
     u32x4 z;
@@ -201,8 +201,7 @@ __device__ inline u32x4 anew<Int8>(u32x4 x, float old, float s) {
         u32 y[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float q = fmaf((float)((u >> (8 * i)) & 0xFFu), ratio, less);
-            const float n = q + kWhole;
+            const float q = fmaf((float)((u >> (8 * i)) & 0xFFu), ratio, less), n = q + kWhole;
             y[i] = __float_as_uint(n);
             off = fmaxf(off, fabsf(q - (n - kWhole)));
         }
@@ -366,13 +365,16 @@ __global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
         if (lane % (64 / PIECES) == 0) tops[turn][wave * PIECES + lane / (64 / PIECES)] = mine_top;
         // all of this round is read, and its maxima are there
         meet();
-        const int group = (D << a.lp) / 1024;  // entries of `tops` to a page
+        const int group = (D << a.lp) / 1024;  // entries of `tops` to a page, a power of two
+        float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const int at = (wave * PIECES + i) / group * group;
-            float m = 0.0f;
-            for (int j = 0; j < group; ++j) m = fmaxf(m, tops[turn][at + j]);
-            const float s = scale_of<C>(m);
+            if (i == 0 || group < PIECES) {  // (a larger page's are all the same)
+                const int at = (wave * PIECES + i) & -group;
+                float m = 0.0f;
+                for (int j = 0; j < group; ++j) m = fmaxf(m, tops[turn][at + j]);
+                s = scale_of<C>(m);
+            }
             __builtin_amdgcn_sched_barrier(0);  // one after the other: registers
             // a piece lies in one page
             const int page = __builtin_amdgcn_readlane(to, i);
@@ -388,10 +390,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
     }
 }
 
-#ifndef KW
-#define KW 16
-#endif
-constexpr int kWaves = KW, kPieces = 64 / KW;
+constexpr int kWaves = 16, kPieces = 4;
 
 template <class C, int D>
 int launch_compact(const CompactArgs &a, int n_requests, void *stream) {

@@ -145,6 +145,30 @@ def test_extreme_scales_and_codes(code):
     moved(s.cuda(), some([512], [200], seed=5))
 
 
+@pytest.mark.parametrize("code", [E4M3, torch.int8], ids=str)
+def test_codes_of_zero_under_scales_of_any_size(code):
+    """0 stays 0 beside the least scales, and one that is 2^20 to 2^200 times as large."""
+    for big in (2.0 ** -80, 1.0, 3e38):
+        s = Setup([64], [1], page=16, kv=1, heads=1, dim=64, code=code, seed=6)
+        pages = s.table[0].long()
+        s.k[pages[1]] = torch.zeros((1, 16, 64)).to(code)
+        s.ks[:] = 2.0 ** -100
+        s.ks[pages[1]] = big
+        moved(s.cuda(), [[0, 2, 16, 17, 30, 40, 50, 60, 61, 62]], where=str(big))
+
+
+def test_scales_many_times_the_new_one():
+    """What had the old scale's large codes is gone: codes of 1, 2, .. grow up to 127 fold, and round as exactly."""
+    g = np.random.default_rng(8)
+    for k in range(12):
+        s = Setup([640], [1], page=16, kv=1, heads=1, dim=64, code=torch.int8, seed=k)
+        pages = s.table[0].long()
+        small = torch.from_numpy(g.integers(-(k + 1), k + 2, (40, 1, 16, 64)).astype(np.int8))
+        s.k[pages] = small
+        s.ks[pages] = torch.from_numpy(g.uniform(0.5, 1.0 + 3 * k, (40, 1)).astype(np.float32))
+        moved(s.cuda(), some([640], [300], seed=k), where=str(k))
+
+
 def test_ties_round_to_even():
     """Scales whose quotients are halves: exact ties, and quotients next to one."""
     s = Setup([64], [1], page=16, kv=1, heads=1, dim=64, code=torch.int8)
