@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -37,6 +38,10 @@ class Lists(ctypes.Structure):
                 ("mask_stride", _i64), ("n_masks", _i32), ("row_mask", _P)]
 
 
+# The same as bytes: made in a third of the time of a ctypes structure, and the short calls' host time counts.
+pack_heads = struct.Struct("@PqqPqqi4x").pack
+pack_lists = struct.Struct("@PPPPPPPPPPqiP").pack
+
 _lib = None
 
 
@@ -49,7 +54,8 @@ def lib():
                              "`python -m paper_2609_08450_amd.build` (no CPU fallback exists)")
         L = ctypes.CDLL(SERVE_LIB_PATH)
         _topk._check_single_hip_runtime()
-        C, R, H, S = (ctypes.POINTER(x) for x in (_paged._Cache, Rotary, Heads, Lists))
+        # (structures as addresses: a call hands Heads and Lists over as packed bytes)
+        C = R = H = S = _P
         L.serve_rotate.argtypes = [_i32, R, _P, _i32, _i32, _i32, H, H, _i32, _P]
         L.serve_weigh_workspace.argtypes = [_i32, _i32, _i32, _i32]
         L.serve_weigh_workspace.restype = _size
@@ -79,3 +85,17 @@ def empty(shape, like, dtype, stream):
         return torch.empty(shape, dtype=dtype, device=like.device)
     with _paged._on(stream):
         return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def vec(t, dtype, n, name, dev):
+    """Address of a contiguous tensor of one axis, of this type and length (None: any), on device `dev`."""
+    if t.dtype is dtype and t.get_device() == dev and t.stride() == (1,) and (n is None or t.shape[0] == n):
+        return t.data_ptr()
+    return _paged._ptr(t, dtype, (n,), name, dev)
+
+
+def flat(t, dtype, shape, name, dev):
+    """Address of a contiguous tensor of this type and shape (None: any), on device `dev`."""
+    if t.dtype is dtype and t.get_device() == dev and (shape is None or t.shape == shape) and t.is_contiguous():
+        return t.data_ptr()
+    return _paged._ptr(t, dtype, t.shape if shape is None else shape, name, dev)

@@ -247,7 +247,7 @@ __device__ float tops_of(float (&t)[N]) {
 // loads that are on their way, too.)
 __device__ inline void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// WAVES of a workgroup hold PIECES of 1024 bytes of codes each, at least a page of 64 KB together.
+// WAVES of a workgroup hold PIECES of 1024 bytes of codes each, at least a page together.
 template <class C, int D, int WAVES, int PIECES>
 __global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
     constexpr int TOKENS = PIECES * 1024 / D;  // of a wave's part
@@ -390,12 +390,15 @@ __global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
     }
 }
 
-constexpr int kWaves = 16, kPieces = 4;
-
 template <class C, int D>
 int launch_compact(const CompactArgs &a, int n_requests, void *stream) {
     const dim3 grid((unsigned)(a.n_heads * a.sides), (unsigned)n_requests);
-    return launch(compact_kernel<C, D, kWaves, kPieces>, grid, dim3(64 * kWaves), stream, a);
+    // 16 waves where workgroups are few, so that one has more on its way (four requests of 604
+    // tokens 12.6 us, and 15.5 with 8 waves); 8 where there are more than the card holds at a time,
+    // so that one computes while another waits (1024 of 4096 tokens 274 us, and 304 with 16)
+    const bool small = (int64_t)grid.x * n_requests >= 512 && (D << a.lp) <= 32768;
+    return small ? launch(compact_kernel<C, D, 8, 4>, grid, dim3(512), stream, a)
+                 : launch(compact_kernel<C, D, 16, 4>, grid, dim3(1024), stream, a);
 }
 
 }  // namespace

@@ -16,9 +16,10 @@ namespace paged {
 namespace {
 
 constexpr int kBlock = 512;
-constexpr u32 kSeen = 0x80000000u;    // of a word: the token is among the row's
+constexpr u32 kSeen = 0x80000000u;    // of a word: the token is among the prompt's
 constexpr u32 kBiased = 0x40000000u;  // it has a bias; below: how often it is behind the prompt
 constexpr int kListed = 128;          // biases of a chunk that are listed in LDS
+constexpr int kAhead = 8;             // tokens of a thread that are on their way at once
 
 struct AdjustArgs {
     const void *x;
@@ -55,8 +56,12 @@ __global__ __launch_bounds__(kBlock) void adjust_kernel(AdjustArgs a) {
     __shared__ alignas(16) u32 words[CHUNK];
     __shared__ Bias listed[kListed];
     __shared__ u32 biased;
-    const int tid = threadIdx.x, row = blockIdx.y;
-    const int first = blockIdx.x * CHUNK, left = min(CHUNK, a.vocab - first);
+    const int tid = threadIdx.x;
+    // the chunks of a row on one XCD (workgroups go round them), whose L2 then holds its lists
+    const int chunks = gridDim.x, b = blockIdx.y * chunks + blockIdx.x, whole = a.n_rows & ~7;
+    const bool round = b < whole * chunks;
+    const int row = round ? b / (8 * chunks) * 8 + b % 8 : blockIdx.y, chunk = round ? b / 8 % chunks : blockIdx.x;
+    const int first = chunk * CHUNK, left = min(CHUNK, a.vocab - first);
     const T *x = (const T *)a.x + row * a.x_row + first;
     // what the row's lists and mask are
     int64_t begin = 0, end = 0, prompt = 0, bias_begin = 0, bias_end = 0;
@@ -98,11 +103,19 @@ __global__ __launch_bounds__(kBlock) void adjust_kernel(AdjustArgs a) {
         for (int i = 4 * tid; i < CHUNK; i += 4 * kBlock) *(u32x4 *)&words[i] = u32x4{0, 0, 0, 0};
         if (tid == 0) biased = 0;
         __syncthreads();
-        for (int64_t i = begin + tid; i < end; i += kBlock) {
-            const u32 at = (u32)a.l.tokens[i] - (u32)first;
-            if (at >= (u32)left) continue;
-            atomicOr(&words[at], kSeen);
-            if (i >= prompt) atomicAdd(&words[at], 1u);
+        // (several tokens of a thread at once: one after the other each would cost a trip to memory)
+        for (int64_t i0 = begin + tid; i0 < end; i0 += kAhead * kBlock) {
+            int token[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) token[j] = a.l.tokens[min(i0 + j * kBlock, end - 1)];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const int64_t i = i0 + j * kBlock;
+                const u32 at = (u32)token[j] - (u32)first;
+                if (i >= end || at >= (u32)left) continue;
+                if (i < prompt) atomicOr(&words[at], kSeen);
+                else atomicAdd(&words[at], 1u);
+            }
         }
         for (int64_t i = bias_begin + tid; i < bias_end; i += kBlock) {
             const u32 at = (u32)a.l.bias_ids[i] - (u32)first;
@@ -144,7 +157,7 @@ __global__ __launch_bounds__(kBlock) void adjust_kernel(AdjustArgs a) {
         for (int j = 0; j < V; ++j) {
             float z = y[j];
             if (w[j]) {
-                if (w[j] & kSeen) z = z > 0.0f ? __fdiv_rn(z, repetition) : z * repetition;
+                if (w[j] & ~kBiased) z = z > 0.0f ? __fdiv_rn(z, repetition) : z * repetition;
                 const u32 n = w[j] & ~(kSeen | kBiased);
                 if (n) {
                     const float by = frequency * (float)n;

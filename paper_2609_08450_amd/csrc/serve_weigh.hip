@@ -606,13 +606,13 @@ extern "C" int serve_weigh(const paged_kv_cache *cache, int32_t act, const void 
         return PAGED_KV_EINVAL;
     if (n_rows == 0 || n_requests == 0) return PAGED_KV_OK;
     if (!q || !lse || !table || !row_starts || !row_lengths || !weights || !weight_offsets || !aligned16(q) ||
-        q_row % 8 || q_head % 8 || !workspace || (uintptr_t)workspace % 256)
+        q_row % 8 || q_head % 8 || (many(n_rows, n_requests) && !workspace) || (uintptr_t)workspace % 256)
         return PAGED_KV_EINVAL;
     const int lp = log2_page(cache->page);
     if (((int64_t)table_width << lp) > 0x7FFFFFFF - 65536 || n_requests > 65535) return PAGED_KV_EUNSUPPORTED;
     const size_t need = serve_weigh_workspace(n_rows, n_requests, heads, cache->n_heads);
     if (need == 0) return PAGED_KV_EUNSUPPORTED;
-    if (workspace_bytes < need) return PAGED_KV_EWORKSPACE;
+    if (many(n_rows, n_requests) && workspace_bytes < need) return PAGED_KV_EWORKSPACE;
     const double exact = (double)scale * 1.4426950408889634;
     const float scale2 = (float)exact;
     BlockArgs b = {};

@@ -26,10 +26,19 @@ from . import topk as _topk
 PagedError = _paged.PagedError
 
 
+_sizes = {}  # bytes by (rows, requests, heads, cache heads)
+
+
 def workspace_size(cache, n_rows: int, n_requests: int, heads: int) -> int:
-    size = _serve.lib().serve_weigh_workspace(n_rows, n_requests, heads, cache.n_heads)
-    if size == 0:
-        raise PagedError("serve_weigh_workspace: invalid arguments or device")
+    key = (n_rows, n_requests, heads, cache.n_heads)
+    size = _sizes.get(key)
+    if size is None:
+        size = _serve.lib().serve_weigh_workspace(*key)
+        if size == 0:
+            raise PagedError("serve_weigh_workspace: invalid arguments or device")
+        if len(_sizes) >= 1024:
+            _sizes.clear()
+        _sizes[key] = size
     return size
 
 
@@ -38,27 +47,31 @@ def weigh(cache, q, lse, table, row_starts, row_lengths, scale: float, weights, 
     """Forwards to serve_weigh(): adds to each request's weights (any contiguous float32 tensor, request r's
     from weight_offsets[r] on) what its tokens got of the attention of q [rows, heads, dim], whose ``lse``
     float32 [rows, heads] ``paged.attend`` gave.  ``workspace``: uint8 of ``workspace_size`` bytes, for a
-    program that keeps one."""
+    program that keeps one; calls of at most one row to a request use none."""
     dev = cache._on_current()
     qp, q_row, q_head = _paged._rows3(q, None, cache.head_dim, "q", dev)
     rows, heads, _ = q.shape
     at, stride, width = _paged._table(table, dev)
     n = table.shape[0]
-    need = workspace_size(cache, rows, n, heads)
-    if workspace is None:
-        workspace = _serve.empty(need, q, torch.uint8, stream)
-    elif workspace.get_device() != dev:
-        raise _paged._elsewhere(workspace, dev, "workspace")
-    elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
-        raise PagedError("workspace must be a contiguous device tensor of uint8")
+    wp = size = 0
+    if workspace is not None:
+        if workspace.get_device() != dev:
+            raise _paged._elsewhere(workspace, dev, "workspace")
+        if workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
+            raise PagedError("workspace must be a contiguous device tensor of uint8")
+        wp, size = workspace.data_ptr(), workspace.numel()
+    elif rows > n:
+        size = workspace_size(cache, rows, n, heads)
+        workspace = _serve.empty(size, q, torch.uint8, stream)
+        wp = workspace.data_ptr()
     _serve.check((_serve._lib or _serve.lib()).serve_weigh(
         cache._ref, _paged.ACTS[q.dtype], qp, q_row, q_head, heads,
-        _paged._ptr(lse, torch.float32, (rows, heads), "lse", dev), at, stride, width,
-        _paged._vec(row_starts, torch.int32, n + 1, "row_starts", dev), n,
-        _paged._vec(row_lengths, torch.int32, rows, "row_lengths", dev), rows, scale,
-        _paged._ptr(weights, torch.float32, weights.shape, "weights", dev),
-        _paged._vec(weight_offsets, torch.int64, n, "weight_offsets", dev), workspace.data_ptr(), workspace.numel(),
-        _topk._stream(stream)), "serve_weigh")
+        _serve.flat(lse, torch.float32, (rows, heads), "lse", dev), at, stride, width,
+        _serve.vec(row_starts, torch.int32, n + 1, "row_starts", dev), n,
+        _serve.vec(row_lengths, torch.int32, rows, "row_lengths", dev), rows, scale,
+        _serve.flat(weights, torch.float32, None, "weights", dev),
+        _serve.vec(weight_offsets, torch.int64, n, "weight_offsets", dev), wp, size, _topk._stream(stream)),
+        "serve_weigh")
 
 
 def keep(idx, lens, first: int, last: int, kept, counts, *, base: int = 0, weights=None, weight_offsets=None,
@@ -75,11 +88,11 @@ def keep(idx, lens, first: int, last: int, kept, counts, *, base: int = 0, weigh
         raise PagedError("weights and weight_offsets belong together")
     wp, op = None, None
     if weights is not None:
-        wp = _paged._ptr(weights, torch.float32, weights.shape, "weights", dev)
-        op = _paged._vec(weight_offsets, torch.int64, n, "weight_offsets", dev)
+        wp = _serve.flat(weights, torch.float32, None, "weights", dev)
+        op = _serve.vec(weight_offsets, torch.int64, n, "weight_offsets", dev)
     _serve.check((_serve._lib or _serve.lib()).serve_keep(
-        at, idx.shape[1], base, _paged._vec(lens, i32, n, "lens", dev), n, first, last,
-        _paged._ptr(kept, i32, (n, None), "kept", dev), kept.shape[1], _paged._vec(counts, i32, n, "counts", dev), wp, op,
+        at, idx.shape[1], base, _serve.vec(lens, i32, n, "lens", dev), n, first, last,
+        _paged._ptr(kept, i32, (n, None), "kept", dev), kept.shape[1], _serve.vec(counts, i32, n, "counts", dev), wp, op,
         _topk._stream(stream)), "serve_keep")
 
 
@@ -91,5 +104,5 @@ def compact(cache, table, kept, counts, stream=None) -> None:
     n = table.shape[0]
     kp = _paged._ptr(kept, torch.int32, (n, None), "kept", dev)
     _serve.check((_serve._lib or _serve.lib()).serve_compact(
-        cache._ref, at, stride, width, kp, kept.shape[1], _paged._vec(counts, torch.int32, n, "counts", dev), n,
+        cache._ref, at, stride, width, kp, kept.shape[1], _serve.vec(counts, torch.int32, n, "counts", dev), n,
         _topk._stream(stream)), "serve_compact")

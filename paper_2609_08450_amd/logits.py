@@ -8,8 +8,6 @@ current one, without a synchronisation or a fallback; errors are ``paged.PagedEr
 """
 from __future__ import annotations
 
-import ctypes
-
 import torch
 
 from . import _serve
@@ -19,15 +17,16 @@ from . import topk as _topk
 PagedError = _paged.PagedError
 
 
-def _rows(t, dtypes, shape, name, dev):
+def _rows(t, ok, shape, what, name, dev):
+    """Address and row stride of a tensor [rows, columns] whose last axis is contiguous."""
+    got, at = t.shape, t.stride()
     if t.get_device() != dev:
         raise _paged._elsewhere(t, dev, name)
-    if t.dtype not in dtypes or (shape is not None and t.shape != shape) or t.dim() != 2:
-        raise PagedError(f"{name} must be {' or '.join(map(str, dtypes))} of shape "
-                         f"{tuple(shape) if shape is not None else '(rows, vocab)'}, got {t.dtype} {tuple(t.shape)}")
-    if t.shape[1] > 1 and t.stride(1) != 1 and t.numel():
+    if not ok or len(got) != 2 or (shape is not None and got != shape):
+        raise PagedError(f"{name} must be {what}, got {t.dtype} {tuple(got)}")
+    if at[1] != 1 and got[1] > 1 and got[0]:
         raise PagedError(f"{name} must have a contiguous last axis")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.data_ptr(), at[0] if got[0] > 1 else got[1]
 
 
 def adjust(x, out=None, *, tokens=None, token_starts=None, prompt_lens=None, repetition=None, frequency=None,
@@ -44,16 +43,15 @@ def adjust(x, out=None, *, tokens=None, token_starts=None, prompt_lens=None, rep
 
     Returns out."""
     dev = _paged._device(x, "x")
-    xp, x_row = _rows(x, _serve.ACTS, None, "x", dev)
-    rows, vocab = x.shape
+    act, i32, i64, f32 = _serve.ACTS.get(x.dtype), torch.int32, torch.int64, torch.float32
+    xp, x_row = _rows(x, act is not None, None, "bfloat16, float16 or float32 [rows, vocab]", "x", dev)
+    rows, vocab = shape = x.shape
     if out is None:
-        out = _serve.empty(x.shape, x, torch.float32, stream)
-    op, out_row = _rows(out, (torch.float32,), x.shape, "out", dev)
+        out = _serve.empty(shape, x, f32, stream)
+    op, out_row = _rows(out, out.dtype is f32, shape, f"float32 of shape {tuple(shape)}", "out", dev)
     if rows > 1 and out_row < vocab:
         raise PagedError("out's rows must not overlap")
-
-    def vec(t, dtype, n, name):
-        return None if t is None else _paged._vec(t, dtype, t.numel() if n is None else n, name, dev)
+    vec = _serve.vec
 
     if (tokens is None) != (token_starts is None):
         raise PagedError("tokens and token_starts belong together")
@@ -61,27 +59,28 @@ def adjust(x, out=None, *, tokens=None, token_starts=None, prompt_lens=None, rep
         raise PagedError("penalties need tokens")
     if not (bias_ids is None) == (bias is None) == (bias_starts is None):
         raise PagedError("bias_ids, bias and bias_starts belong together")
-    if bias is not None and bias.numel() != bias_ids.numel():
-        raise PagedError("bias_ids and bias must have one length")
     if row_mask is not None and mask is None:
         raise PagedError("row_mask belongs to a mask")
-    mp, stride, masks = None, 0, 0
+    mp = stride = masks = 0
     if mask is not None:
-        mp, stride = _rows(mask, (torch.int32,), None, "mask", dev)
+        mp, stride = _rows(mask, mask.dtype is i32, None, "int32 [masks, words]", "mask", dev)
         masks, words = mask.shape
         if words * 32 < vocab:
             raise PagedError(f"mask must have {(vocab + 31) // 32} words, got {words}")
         if row_mask is None and masks != rows:
             raise PagedError(f"{masks} masks for {rows} rows need a row_mask")
-    i32, i64, f32 = torch.int32, torch.int64, torch.float32
-    # an empty list has no address, and is none
-    lists = _serve.Lists(vec(tokens, i32, None, "tokens"), vec(token_starts, i64, rows + 1, "token_starts"),
-                         vec(prompt_lens, i32, rows, "prompt_lens"), vec(repetition, f32, rows, "repetition"),
-                         vec(frequency, f32, rows, "frequency"), vec(presence, f32, rows, "presence"),
-                         vec(bias_ids, i32, None, "bias_ids"), vec(bias, f32, None, "bias"),
-                         vec(bias_starts, i64, rows + 1, "bias_starts"), mp, stride, masks,
-                         vec(row_mask, i32, rows, "row_mask"))
+    # (an empty list has no address, and is none)
+    lists = _serve.pack_lists(
+        0 if tokens is None else vec(tokens, i32, None, "tokens", dev),
+        0 if tokens is None else vec(token_starts, i64, rows + 1, "token_starts", dev),
+        0 if prompt_lens is None else vec(prompt_lens, i32, rows, "prompt_lens", dev),
+        0 if repetition is None else vec(repetition, f32, rows, "repetition", dev),
+        0 if frequency is None else vec(frequency, f32, rows, "frequency", dev),
+        0 if presence is None else vec(presence, f32, rows, "presence", dev),
+        0 if bias_ids is None else vec(bias_ids, i32, None, "bias_ids", dev),
+        0 if bias_ids is None else vec(bias, f32, bias_ids.shape[0], "bias", dev),
+        0 if bias_ids is None else vec(bias_starts, i64, rows + 1, "bias_starts", dev),
+        mp, stride, masks, 0 if row_mask is None else vec(row_mask, i32, rows, "row_mask", dev))
     _serve.check((_serve._lib or _serve.lib()).serve_adjust(
-        _serve.ACTS[x.dtype], xp, x_row, op, out_row, rows, vocab, ctypes.byref(lists), _topk._stream(stream)),
-        "serve_adjust")
+        act, xp, x_row, op, out_row, rows, vocab, lists, _topk._stream(stream)), "serve_adjust")
     return out

@@ -107,34 +107,42 @@ class Rotary:
         self.turns = torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in turns], dtype=torch.int64, device=device)
         self._device = self.turns.get_device()
         self._c = _serve.Rotary(self.turns.data_ptr(), self.magnitude, self.rot, start, LAYOUTS[layout])
-        self._ref = ctypes.byref(self._c)
+        self._at = ctypes.addressof(self._c)
+
+
+def _check_heads(x, name, dtype, shape, dev):
+    """What makes heads [rows, heads, dim] unfit."""
+    if x.get_device() != dev:
+        raise _paged._elsewhere(x, dev, name)
+    if x.dtype is not dtype or tuple(x.shape) != shape:
+        raise PagedError(f"{name} must be {dtype} of shape {shape}, got {x.dtype} {tuple(x.shape)}")
+    if x.numel() and shape[2] > 1 and x.stride(2) != 1:
+        raise PagedError(f"{name} must have a contiguous last axis")
 
 
 def _heads(x, out, name, dtype, rows, dim, dev, stream):
-    if x.get_device() != dev:
-        raise _paged._elsewhere(x, dev, name)
-    if x.dtype is not dtype or x.dim() != 3 or x.shape[0] != rows or x.shape[2] != dim:
-        raise PagedError(f"{name} must be {dtype} of shape ({rows}, heads, {dim}), got {x.dtype} {tuple(x.shape)}")
-    if out is None:
-        out = _serve.empty(x.shape, x, dtype, stream)
-    elif out is not x:
-        if out.get_device() != dev:
-            raise _paged._elsewhere(out, dev, name + "_out")
-        if out.dtype is not dtype or out.shape != x.shape:
-            raise PagedError(f"{name}_out must be {dtype} of shape {tuple(x.shape)}, got {out.dtype} {tuple(out.shape)}")
-    for t, what in ((x, name), (out, name + "_out")):
-        if dim > 1 and t.stride(2) != 1 and t.numel():
-            raise PagedError(f"{what} must have a contiguous last axis")
-    _distinct(out, name + "_out")
-    one_row, one_head = x.shape[0] == 1, x.shape[1] == 1
-    strides = [0 if one else t.stride(i) for t in (x, out) for i, one in ((0, one_row), (1, one_head))]
-    return out, _serve.Heads(x.data_ptr(), strides[0], strides[1], out.data_ptr(), strides[2], strides[3], x.shape[1])
-
-
-def _distinct(t, name):
-    """Refuses an output whose elements share memory (an expanded tensor)."""
-    if t.numel() and any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())):
-        raise PagedError(f"{name} must not be an expanded tensor")
+    """The output, and serve_heads as bytes."""
+    shape, at = x.shape, x.stride()
+    if x.get_device() != dev or x.dtype is not dtype or len(shape) != 3 or shape[0] != rows or shape[2] != dim or at[2] != 1:
+        _check_heads(x, name, dtype, (rows, shape[1] if len(shape) == 3 else "heads", dim), dev)
+    heads = shape[1]
+    if out is x:
+        to = at
+    elif out is None:
+        out = _serve.empty(shape, x, dtype, stream)
+        to = (heads * dim, dim, 1)
+    else:
+        to = out.stride()
+        if out.get_device() != dev or out.dtype is not dtype or out.shape != shape or to[2] != 1:
+            _check_heads(out, name + "_out", dtype, tuple(shape), dev)
+    if 0 in to and any(n > 1 and s == 0 for n, s in zip(shape, to)) and x.numel():
+        raise PagedError(f"{name}_out must not be an expanded tensor")
+    row, head, to_row, to_head = at[0], at[1], to[0], to[1]
+    if rows == 1:  # the stride of an axis of length one says nothing
+        row = to_row = 0
+    if heads == 1:
+        head = to_head = 0
+    return out, _serve.pack_heads(x.data_ptr(), row, head, out.data_ptr(), to_row, to_head, heads)
 
 
 def rotate(rotary: Rotary, positions, q, k=None, *, q_out=None, k_out=None, transposed: bool = False, stream=None):
@@ -145,18 +153,19 @@ def rotate(rotary: Rotary, positions, q, k=None, *, q_out=None, k_out=None, tran
     dev = _paged._device(q, "q")
     if rotary._device != dev:
         raise PagedError(f"the rotary frequencies are on cuda:{rotary._device}, q is on cuda:{dev}")
-    if q.dtype not in _serve.ACTS or q.dim() != 3:
-        raise PagedError(f"q must be bfloat16, float16 or float32 [rows, heads, dim], got {q.dtype} {tuple(q.shape)}")
-    rows, _, dim = q.shape
+    dtype, shape = q.dtype, q.shape
+    act = _serve.ACTS.get(dtype)
+    if act is None or len(shape) != 3:
+        raise PagedError(f"q must be bfloat16, float16 or float32 [rows, heads, dim], got {dtype} {tuple(shape)}")
+    rows, _, dim = shape
     wide = positions.dtype is torch.int64
-    at = _paged._vec(positions, torch.int64 if wide else torch.int32, rows, "positions", dev)
-    q_out, qh = _heads(q, q_out, "q", q.dtype, rows, dim, dev, stream)
+    at = _serve.vec(positions, torch.int64 if wide else torch.int32, rows, "positions", dev)
+    q_out, qh = _heads(q, q_out, "q", dtype, rows, dim, dev, stream)
     kh = None
     if k is not None:
-        k_out, kh = _heads(k, k_out, "k", q.dtype, rows, dim, dev, stream)
+        k_out, kh = _heads(k, k_out, "k", dtype, rows, dim, dev, stream)
     elif k_out is not None:
         raise PagedError("k_out belongs to a k")
     _serve.check((_serve._lib or _serve.lib()).serve_rotate(
-        _serve.ACTS[q.dtype], rotary._ref, at, wide, rows, dim, ctypes.byref(qh),
-        ctypes.byref(kh) if kh is not None else None, transposed, _topk._stream(stream)), "serve_rotate")
+        act, rotary._at, at, wide, rows, dim, qh, kh, transposed, _topk._stream(stream)), "serve_rotate")
     return q_out if k is None else (q_out, k_out)

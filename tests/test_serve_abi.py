@@ -46,6 +46,13 @@ def test_structures_mirror_the_header(serve, name, mirror):
     assert [(n, kinds[k]) for n, k in fields] == [(n.rstrip("_"), t) for n, t in getattr(serve, mirror)._fields_]
 
 
+def test_packed_structures_are_the_same_bytes(serve):
+    heads = (1 << 40, 3, -4, 5, 6, 7, 8)
+    assert serve.pack_heads(*heads) == bytes(serve.Heads(*heads))
+    lists = (1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13)
+    assert serve.pack_lists(*lists) == bytes(serve.Lists(*lists))
+
+
 def test_constants_mirror_the_header(serve):
     assert serve.ACTS[torch.float32] == int(re.search(r"#define SERVE_F32 (\d+)", TEXT).group(1))
     assert len(serve.ACTS) == 3
