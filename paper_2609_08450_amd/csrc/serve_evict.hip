@@ -384,7 +384,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
             const float was = scale_at(i);
             const u32x4 y = was == s ? x[i] : anew<C>(x[i], was, s);
             const u32 row = (u32)page * a.page_rows + head_row + (u32)(t & (P - 1));
-            if (t + 16 * lane / D < count) *(u32x4 *)(codes + (int64_t)row * D + 16 * lane) = y;
+            if (t + 16 * lane / D < count) __builtin_nontemporal_store(y, (u32x4 *)(codes + (int64_t)row * D + 16 * lane));
             if ((t & (P - 1)) == 0 && lane == 0) scales[page * a.scale_stride] = s;
         }
     }
