@@ -185,36 +185,53 @@ __global__ __launch_bounds__(kBlock) void weigh_rows_kernel(WeighArgs a) {
         }
 }
 
-// Many rows.  A chunk is the queries of some rows to one cache head, up to 64 columns; a
-// request's tiles of tokens each meet its heads' chunks, counted head by head.  A unit is a tile
-// with a piece of up to `size` of these; a tile in several pieces has a part of its sums from
-// each, which a launch of its own joins in order.  Units of one piece follow each other: what
-// runs at a time reads the same queries.
+// Many rows.  A window is the queries of some rows to one cache head, up to 256 columns
+// (128 of heads of 256), which stay in LDS while tokens pass by: every wave has its own, in
+// registers, and no wave waits for another.  A step is 256 tokens of a request; its sums over one
+// window are a part, and a launch of its own joins the parts of a step in order.
+//
+// The steps that windows see, window by window, are laid out in one line and cut into equal shares,
+// one to a resident workgroup: each loads queries twice or three times, however many there are.
+// Where the parts would be more than the workspace holds, several windows make a piece
+// that adds up in one part, and units of a piece and 8 steps are dealt to workgroups as these come free.
 
-constexpr int kPlan = 1024;
-constexpr int kChunk = 64;
-constexpr int kUnits = 9216;  // about so many units to a call: 12 to a resident workgroup
-constexpr int kLeast = 8;     // chunks of a unit, where there are so many
+constexpr int kPlan = 512;
+constexpr int kRange = 8;      // steps of a unit
+constexpr int kParts = 49152;  // parts of a call: 50 MB
+
+// Columns of a window.
+constexpr int window_of(int dim) { return dim == 256 ? 128 : 256; }
+
+struct Request {
+    int64_t base;     // what is dealt out before its own: steps that windows see, or units
+    int longest;      // of its rows
+    int window_base;  // its windows of a head, before all heads
+    int part_base;    // parts before its own: of each of its pieces, all steps
+    int step_base;    // steps that lie in parts before its own
+    int row0, row1;
+};
 
 struct Plan {
-    int64_t *unit_base;  // [n + 1] prefix sum of the requests' units
-    int *counter;        // units taken
-    int *size;           // chunks of a unit
-    int *slot_base;      // [n + 1] of the parts
-    int *tile_base;      // [n + 1] of the tiles that lie in parts
-    int *chunk_base;     // [n + 1] of the chunks of a head
-    int *longest;        // [n]
-    int *chunk_max, *chunk_min;  // [max_chunks] lengths of a chunk's rows
-    float *parts;        // [2 * kUnits][kTile]
+    Request *requests;  // [n + 1]
+    int *counter;       // units taken
+    int *size;          // windows of a piece
+    int *window_max, *window_min;  // [max_windows] lengths of a window's rows
+    int *window_steps;  // [max_windows] steps that the windows before it see, of its request
+    float *parts;       // [kParts][kTile]
 };
 
 struct BlockArgs {
     WeighArgs a;
-    int n, rows, parts;  // requests; rows of a chunk; chunks of a row, where a head's queries are more than a chunk
-    int max_chunks;
+    int n, rows, parts;  // requests; rows of a window; windows of a row, where a head's queries are more than a window
+    int max_windows;
+    u32 page_rows;    // rows of head_dim codes from one page to the next
+    u32 per_inverse;  // 65536 / per, rounded up: a column's row without a division
+    int skip_heads;   // from one column of a thread to its next: heads (of the row it comes to),
+    int64_t skip, wrap;  // bytes of q, and bytes more where the head is past the row's last
     Plan p;
 };
 
+__device__ inline int steps_of(int len) { return (int)(((int64_t)len + kTile - 1) / kTile); }
 __device__ inline int bounded(const WeighArgs &a, int r) { return min(max(a.row_starts[r], 0), a.n_rows); }
 
 // Exclusive prefix of x over the workgroup; total in *sum.
@@ -237,327 +254,600 @@ __device__ int64_t prefix(int64_t x, int64_t *waves, int64_t *sum) {
     return before + s - x;
 }
 
-// Last i in [0, n) with base[i] <= x (base rises, base[0] <= x).
-template <class I>
-__device__ int last_base(const I *base, int n, int64_t x) {
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (base[mid] <= x) lo = mid; else hi = mid;
+// Last i in [0, n) with base(i) <= x (base rises, base(0) <= x), the wave's lanes looking at 64 at once.
+template <class F>
+__device__ int last_base(int n, int64_t x, F base) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0;
+    while (n > 1) {
+        const int step = (n + 63) / 64;
+        const uint64_t m = __ballot(lane * step < n && base(lo + min(lane * step, n - 1)) <= x);
+        const int at = (63 - __builtin_clzll(m)) * step;
+        lo += at;
+        n = min(step, n - at);
     }
-    return lo;
+    return __builtin_amdgcn_readfirstlane(lo);
 }
 
 __global__ __launch_bounds__(kPlan) void plan_kernel(BlockArgs b) {
     __shared__ int64_t waves[kPlan / 64];
+    __shared__ int first[kPlan + 1], most_of[kPlan];  // of a round: windows before a request's, its longest row
+    __shared__ unsigned long long seen_by[kPlan];     // steps that its windows see, then those of the requests before
     const WeighArgs &a = b.a;
     const Plan &p = b.p;
     const int tid = threadIdx.x;
     const int64_t cap = (int64_t)a.table_width << a.lp;
-    int64_t base = 0, all = 0;
+    int64_t windows = 0, work = 0, all = 0;
     for (int r0 = 0; r0 < b.n; r0 += kPlan) {
-        const int r = r0 + tid;
-        int64_t chunks = 0;
+        const int r = r0 + tid, here = min(kPlan, b.n - r0);
+        int row0 = 0, row1 = 0;
         if (r < b.n) {
-            const int rows = max(bounded(a, r + 1) - bounded(a, r), 0);
-            chunks = b.parts > 1 ? (int64_t)rows * b.parts : (rows + b.rows - 1) / b.rows;
-            p.longest[r] = 0;
+            row0 = bounded(a, r);
+            row1 = max(bounded(a, r + 1), row0);
         }
-        const int64_t at = min(base + prefix(chunks, waves, &all), (int64_t)b.max_chunks);
-        if (r < b.n) p.chunk_base[r] = (int)at;
-        base += all;
-    }
-    const int chunks = (int)min(base, (int64_t)b.max_chunks);
-    if (tid == 0) p.chunk_base[b.n] = chunks;
-    __syncthreads();
-    for (int c = tid; c < chunks; c += kPlan) {
-        const int r = last_base(p.chunk_base, b.n, c), i = c - p.chunk_base[r];
-        const int from = bounded(a, r) + (b.parts > 1 ? i / b.parts : i * b.rows);
-        const int to = min(from + (b.parts > 1 ? 1 : b.rows), bounded(a, r + 1));
-        int most = 0, least = 0x7FFFFFFF;
-        for (int row = from; row < to; row += 8) {
-            int len[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) len[j] = a.row_lengths[min(row + j, to - 1)];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                most = max(most, len[j]);
-                least = min(least, max(len[j], 0));
+        const int64_t mine = b.parts > 1 ? (int64_t)(row1 - row0) * b.parts : (row1 - row0 + b.rows - 1) / b.rows;
+        const int from = (int)min(windows + prefix(mine, waves, &all), (int64_t)b.max_windows);
+        first[tid] = from;
+        most_of[tid] = 0;
+        seen_by[tid] = 0;
+        windows = min(windows + all, (int64_t)b.max_windows);
+        if (tid == 0) first[here] = (int)windows;  // (thread `here`, if there is one, writes the same)
+        __syncthreads();
+        // the lengths of a window's rows: 16 lanes to a window
+        for (int w0 = first[0] + tid / 16; w0 < (int)windows; w0 += kPlan / 16) {
+            int lo = 0, hi = here;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (first[mid] <= w0) lo = mid; else hi = mid;
+            }
+            const int i = w0 - first[lo], start = bounded(a, r0 + lo), stop = bounded(a, r0 + lo + 1);
+            const int at = start + (b.parts > 1 ? i / b.parts : i * b.rows);
+            const int end = min(at + (b.parts > 1 ? 1 : b.rows), stop);
+            int most = 0, least = 0x7FFFFFFF;
+#pragma unroll 4
+            for (int row = at + tid % 16; row < end; row += 16) {
+                const int len = (int)min((int64_t)max(a.row_lengths[row], 0), cap);
+                most = max(most, len);
+                least = min(least, len);
+            }
+            for (int d = 8; d; d >>= 1) {
+                most = max(most, __shfl_xor(most, d));
+                least = min(least, __shfl_xor(least, d));
+            }
+            if (tid % 16 == 0) {
+                p.window_max[w0] = most;
+                p.window_min[w0] = least;
+                atomicMax(&most_of[lo], most);
+                atomicAdd(&seen_by[lo], (unsigned long long)steps_of(most));
             }
         }
-        most = (int)min((int64_t)most, cap);
-        least = (int)min((int64_t)least, cap);
-        p.chunk_max[c] = most;
-        p.chunk_min[c] = least;
-        atomicMax(&p.longest[r], most);
-    }
-    __syncthreads();
-    const auto tiles_of = [&](int r) { return ((int64_t)p.longest[r] + kTile - 1) / kTile; };
-    const auto chunks_of = [&](int r) { return (int64_t)(p.chunk_base[r + 1] - p.chunk_base[r]) * a.kv_heads; };
-    int64_t work = 0;
-    for (int r0 = 0; r0 < b.n; r0 += kPlan) {
-        const int r = r0 + tid;
-        prefix(r < b.n ? tiles_of(r) * chunks_of(r) : 0, waves, &all);
+        __syncthreads();
+        const int count = first[min(tid + 1, here)] - from;
+        prefix(r < b.n ? (int64_t)steps_of(most_of[tid]) * count * a.kv_heads : 0, waves, &all);
         work += all;
+        // (the second round puts in the bases: until then what it needs for them)
+        if (r < b.n) p.requests[r] = {(int64_t)seen_by[tid], most_of[tid], from, count, 0, row0, row1};
+        __syncthreads();
+        const unsigned long long before = prefix((int64_t)seen_by[tid], waves, &all);
+        __syncthreads();
+        seen_by[tid] = before;
+        __syncthreads();
+        // the steps that windows before a window see: a line over all requests of the round, less what is before its own
+        int64_t line = 0;
+        for (int w0 = first[0]; w0 < (int)windows; w0 += kPlan) {
+            const int w = w0 + tid;
+            int64_t steps = 0;
+            if (w < (int)windows) steps = steps_of(p.window_max[w]);
+            const int64_t at = line + prefix(steps, waves, &all);
+            line += all;
+            if (w < (int)windows) {
+                int lo = 0, hi = here;
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (first[mid] <= w) lo = mid; else hi = mid;
+                }
+                p.window_steps[w] = (int)min(at - (int64_t)seen_by[lo], (int64_t)0x7FFFFFFF);
+            }
+        }
+        __syncthreads();
     }
-    const int64_t size = max((work + kUnits - 1) / kUnits, (int64_t)kLeast);
-    int64_t units = 0, slots = 0, tiles = 0;
+    // all parts fit: pieces of one window; else of so many that half of them would
+    const int64_t size = work <= kParts ? 1 : (2 * work + kParts - 1) / kParts;
+    int64_t dealt = 0, parts = 0, joined = 0;
     for (int r0 = 0; r0 < b.n; r0 += kPlan) {
         const int r = r0 + tid;
-        int64_t mine = 0, pieces = 0;
+        Request q = {};
+        int64_t mine = 0, in_parts = 0, steps = 0;
         if (r < b.n) {
-            pieces = (chunks_of(r) + size - 1) / size;
-            mine = tiles_of(r) * pieces;
+            q = p.requests[r];
+            const int64_t pieces = ((int64_t)q.part_base * a.kv_heads + size - 1) / size;
+            steps = steps_of(q.longest);
+            mine = size == 1 ? q.base * a.kv_heads : pieces * ((steps + kRange - 1) / kRange);
+            if (pieces > 1) in_parts = pieces * steps;
+            else steps = 0;
         }
-        const int64_t at = units + prefix(mine, waves, &all);
-        units += all;
-        const int64_t slot = slots + prefix(pieces > 1 ? mine : 0, waves, &all);
-        slots += all;
-        const int64_t tile = tiles + prefix(pieces > 1 ? tiles_of(r) : 0, waves, &all);
-        tiles += all;
-        if (r < b.n) {
-            p.unit_base[r] = at;
-            p.slot_base[r] = (int)slot;
-            p.tile_base[r] = (int)tile;
-        }
+        q.base = dealt + prefix(mine, waves, &all);
+        dealt += all;
+        q.part_base = (int)(parts + prefix(in_parts, waves, &all));
+        parts += all;
+        q.step_base = (int)(joined + prefix(steps, waves, &all));
+        joined += all;
+        if (r < b.n) p.requests[r] = q;
     }
     if (tid == 0) {
-        p.unit_base[b.n] = units;
-        p.slot_base[b.n] = (int)slots;
-        p.tile_base[b.n] = (int)tiles;
+        p.requests[b.n] = {dealt, 0, (int)windows, (int)parts, (int)joined, 0, 0};
         *p.size = (int)min(size, (int64_t)0x7FFFFFFF);
         *p.counter = 0;
     }
 }
 
-// One buffer of a chunk.
 template <int D>
-struct Chunk {
-    alignas(16) uint8_t q[kChunk][2 * D + 16];
-    alignas(16) float lse2[kChunk], fine[kChunk];
-    alignas(16) int len[kChunk];
+struct Window {
+    alignas(16) float lse2[window_of(D)], fine[window_of(D)];  // first: their offsets fit the instructions that load them
+    alignas(16) int len[window_of(D)];
+    alignas(16) uint8_t q[window_of(D)][2 * D + 16];
 };
+
+// The softmaxes of 32 columns: place i of half g is column 8 (i / 4) + 4 g + i % 4.
+struct Softmaxes {
+    f32x4 l[4], f[4];
+    template <int D>
+    __device__ void load(const Window<D> &o, int col0) {
+        const int g = (threadIdx.x & 63) >> 5;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            l[i] = *(const f32x4 *)&o.lse2[col0 + 8 * i + 4 * g];
+            f[i] = *(const f32x4 *)&o.fine[col0 + 8 * i + 4 * g];
+        }
+    }
+    __device__ void add(const f32x16 &y, float scale, float &sum) const {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum = fmaf(exp2_(fmaf(y[i], scale, -l[i / 4][i % 4])), f[i / 4][i % 4], sum);
+    }
+};
+
+__device__ inline f32x16 zero16() {
+    f32x16 y;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = 0.0f;
+    return y;
+}
+
+// The products of 32 columns with the wave's 64 tokens, in two phases of eight groups: phase 0 makes
+// those with its second 32 tokens beside the exponentials of the first, phase 1 those of the next 32
+// columns with the first ones beside the exponentials of the second.  The order is written down, since the
+// compiler would put the products first and the vector work behind them: a group holds one matrix
+// instruction, and as much vector work as takes its time, on results that no instruction in flight still
+// writes.  Result i of a phase is scaled in group at(i), raised in the next and added in the one after, which for
+// the last ones is in the phase that follows.  A softmax is loaded as soon as its place is free.
+template <int D, class T>
+struct Pass {
+    typedef typename Act<T>::frag frag;
+    static constexpr int N = D / 16;  // matrix instructions of a product
+    const Window<D> &o;
+    const frag (&k)[kTokens][N];
+    const uint8_t *q;
+    const float *soft;
+    float scale, sum[2], t[16], e[16];
+    frag x[N];
+    f32x16 y[2];
+    f32x4 l[4], f[4];
+
+    static constexpr int at(int i) { return i < 3 ? 1 : i >= 13 ? 7 : (i + 1) / 2; }
+
+    __device__ Pass(const Window<D> &o, const frag (&k)[kTokens][N], float scale) : o(o), k(k), scale(scale) {
+        const int lane = threadIdx.x & 63;
+        q = o.q[lane & 31] + 32 * (lane >> 5);
+        soft = o.lse2 + 4 * (lane >> 5);
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = query(0, j);
+        y[0] = zero16();
+#pragma unroll
+        for (int j = 0; j < N; ++j) y[0] = Act<T>::mfma32(x[j], k[0][j], y[0]);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            l[v] = lse2(0, v);
+            f[v] = fine(0, v);
+        }
+        sum[0] = sum[1] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            t[i] = -__builtin_inff();
+            e[i] = 0.0f;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    __device__ frag query(int col0, int j) const {
+        return __builtin_bit_cast(frag, *(const u32x4 *)(q + col0 * (2 * D + 16) + 64 * (j >> 1) + 16 * (j & 1)));
+    }
+    // place i of half g is column 8 (i / 4) + 4 g + i % 4
+    __device__ f32x4 lse2(int col0, int v) const { return *(const f32x4 *)(soft + col0 + 8 * v); }
+    __device__ f32x4 fine(int col0, int v) const { return *(const f32x4 *)(soft + window_of(D) + col0 + 8 * v); }
+
+    // The vector work of a phase's group.
+    __device__ void work(int phase, int g) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if (at(i) + 2 == g) sum[phase] = fmaf(e[i], f[i / 4][i % 4], sum[phase]);
+            if (at(i) - 6 == g) sum[phase ^ 1] = fmaf(e[i], f[i / 4][i % 4], sum[phase ^ 1]);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (at(i) + 1 == g || at(i) - 7 == g) e[i] = exp2_(t[i]);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (at(i) == g) t[i] = fmaf(y[phase][i], scale, -l[i / 4][i % 4]);
+    }
+    // 32 columns from col0 on; `next` follow, if MORE.
+    template <bool MORE>
+    __device__ void columns(int col0, int next) {
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+            if (g % (8 / (N < 8 ? N : 8)) == 0) {
+                constexpr int EACH = N > 8 ? N / 8 : 1;
+#pragma unroll
+                for (int h = 0; h < EACH; ++h) {
+                    const int j = g / (8 / (N < 8 ? N : 8)) * EACH + h;
+                    y[1] = Act<T>::mfma32(x[j], k[1][j], j == 0 ? zero16() : y[1]);
+                    if (MORE) x[j] = query(next, j);
+                }
+            }
+            work(0, g);
+            // what the columns before have left their places to
+            if (g == 0) l[3] = lse2(col0, 3);
+            if (g == 1) f[2] = fine(col0, 2);
+            if (g == 2) f[3] = fine(col0, 3);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+            if (MORE && g % (8 / (N < 8 ? N : 8)) == 0) {
+                constexpr int EACH = N > 8 ? N / 8 : 1;
+#pragma unroll
+                for (int h = 0; h < EACH; ++h) {
+                    const int j = g / (8 / (N < 8 ? N : 8)) * EACH + h;
+                    y[0] = Act<T>::mfma32(x[j], k[0][j], j == 0 ? zero16() : y[0]);
+                }
+            }
+            work(1, g);
+            if (MORE) {
+                if (g == 3) l[0] = lse2(next, 0);
+                if (g == 5) {
+                    f[0] = fine(next, 0);
+                    l[1] = lse2(next, 1);
+                }
+                if (g == 7) {
+                    f[1] = fine(next, 1);
+                    l[2] = lse2(next, 2);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    // What the last phase has left.
+    __device__ void finish() {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if (at(i) == 7) e[i] = exp2_(t[i]);
+            if (at(i) >= 6) sum[1] = fmaf(e[i], f[i / 4][i % 4], sum[1]);
+        }
+    }
+};
+
+// A window of `cols` columns (a multiple of 32), every row of which sees all of the wave's tokens.
+template <int D, class T>
+__device__ inline void pass(const Window<D> &o, int cols, const typename Act<T>::frag (&k)[kTokens][D / 16], float scale,
+                            float (&sum)[kTokens]) {
+    static_assert(kTokens == 2, "two products for 32 columns");
+    if constexpr (D == 256) {
+        // (the keys take half of the registers: nothing runs ahead)
+        const int lane = threadIdx.x & 63;
+#pragma unroll 1
+        for (int c0 = 0; c0 < cols; c0 += 32) {
+            f32x16 y[kTokens] = {zero16(), zero16()};
+            const uint8_t *q = o.q[c0 + (lane & 31)] + 32 * (lane >> 5);
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) {
+                const auto x = __builtin_bit_cast(typename Act<T>::frag, *(const u32x4 *)(q + 64 * (j >> 1) + 16 * (j & 1)));
+#pragma unroll
+                for (int t = 0; t < kTokens; ++t) y[t] = Act<T>::mfma32(x, k[t][j], y[t]);
+            }
+            Softmaxes c;
+            c.load(o, c0);
+#pragma unroll
+            for (int t = 0; t < kTokens; ++t) c.add(y[t], scale, sum[t]);
+        }
+    } else {
+        Pass<D, T> p(o, k, scale);
+#pragma unroll 1
+        for (int c0 = 0; c0 < cols - 32; c0 += 32) p.template columns<true>(c0, c0 + 32);
+        p.template columns<false>(cols - 32, 0);
+        p.finish();
+#pragma unroll
+        for (int t = 0; t < kTokens; ++t) sum[t] += p.sum[t];
+    }
+}
+
+// Any window, rows that see a part of the tokens among them.
+template <int D, class T>
+__device__ inline void pass_masked(const Window<D> &o, int cols, const typename Act<T>::frag (&k)[kTokens][D / 16],
+                                   float scale, float (&sum)[kTokens], int tok) {
+    const int lane = threadIdx.x & 63, g = lane >> 5;
+#pragma unroll 1
+    for (int c0 = 0; c0 < cols; c0 += 32) {
+        const uint8_t *q = o.q[c0 + (lane & 31)] + 32 * g;
+        f32x16 y[kTokens];
+#pragma unroll
+        for (int t = 0; t < kTokens; ++t) y[t] = zero16();
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+            const auto x = __builtin_bit_cast(typename Act<T>::frag, *(const u32x4 *)(q + 64 * (j >> 1) + 16 * (j & 1)));
+#pragma unroll
+            for (int t = 0; t < kTokens; ++t) y[t] = Act<T>::mfma32(x, k[t][j], y[t]);
+        }
+        Softmaxes c;
+        c.load(o, c0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int len = o.len[c0 + 8 * (i / 4) + 4 * g + i % 4];
+#pragma unroll
+            for (int t = 0; t < kTokens; ++t) {
+                const float p = exp2_(fmaf(y[t][i], scale, -c.l[i / 4][i % 4])) * c.f[i / 4][i % 4];
+                sum[t] += tok + t < len ? p : 0.0f;
+            }
+        }
+    }
+}
 
 template <int D, class T, class C>
-__global__ __launch_bounds__(kBlock, D == 256 ? 2 : 3) void weigh_block_kernel(BlockArgs b) {
-    constexpr int NT = kTokens, PIECES = D / 8 / 4;  // 16-byte pieces of a thread: four threads to a column
+__global__ __launch_bounds__(kBlock, 2) void weigh_block_kernel(BlockArgs b) {
+    constexpr int NT = kTokens, PER = D / 8;  // 16-byte pieces of a column
     typedef typename Act<T>::frag frag;
-    __shared__ Chunk<D> buf[2];
-    __shared__ int64_t taken;
+    __shared__ Window<D> o;
+    __shared__ int taken;
     const WeighArgs &a = b.a;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, g = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
     const int64_t cap = (int64_t)a.table_width << a.lp;
-    const int size = *b.p.size;
-    const int64_t total = b.p.unit_base[b.n];
-    // this thread's column of every chunk
-    const int col = tid >> 2;
-    const int crow = b.parts > 1 ? 0 : col / a.per, chead = b.parts > 1 ? col : col - crow * a.per;
-    const int part_heads = b.parts > 1 ? (a.per + b.parts - 1) / b.parts : a.per;
+    const int size = *b.p.size, window_heads = (a.per + b.parts - 1) / b.parts;
+    const int64_t total = b.p.requests[b.n].base;
 
+    // In equal shares, neighbouring ones, which read the same keys, on one XCD (workgroups go round them).
+    const int eighth = gridDim.x / 8, i8 = blockIdx.x;
+    const int share = i8 < 8 * eighth ? (i8 % 8) * eighth + i8 / 8 : i8;
+    int64_t next = total * share / gridDim.x;
+    const int64_t stop = total * (share + 1) / gridDim.x;
+    int ahead = 0;
+    if (size > 1 && tid == 0) ahead = atomicAdd(b.p.counter, 1);
     for (;;) {
-        __syncthreads();
-        if (tid == 0) taken = atomicAdd(b.p.counter, 1);
-        __syncthreads();
-        const int64_t unit = taken;
-        if (unit >= total) return;
-        const int r = last_base(b.p.unit_base, b.n, unit);
-        const int longest = b.p.longest[r], tiles = (longest + kTile - 1) / kTile;
-        const int i = (int)(unit - b.p.unit_base[r]), piece = i / tiles, tile = i - piece * tiles;
-        const int first_chunk = b.p.chunk_base[r], chunks = b.p.chunk_base[r + 1] - first_chunk;
-        const int64_t all = (int64_t)chunks * a.kv_heads;
-        const int64_t from = (int64_t)piece * size, to = min(from + size, all);
-        const int row0 = bounded(a, r), row1 = bounded(a, r + 1);
-        const int tile0 = tile * kTile, base = tile0 + 32 * NT * wave, tok = base + NT * n;
-        const int pg = a.table[(int64_t)r * a.table_stride + (min((int64_t)tok, cap - 1) >> a.lp)];
-        const bool there = pg >= 0 && pg < a.n_pages;
-        const uint8_t *codes = a.k + (there ? pg : 0) * a.page_stride + (int64_t)(tok & ((1 << a.lp) - 1)) * D + 16 * g;
-        const float *scales = a.ks + (there ? pg : 0) * a.scale_stride;
-        float sum[NT];
+        // the request, its windows [from, to), counted head by head, and steps [s0, s1)
+        if (size > 1) {
+            __syncthreads();
+            if (tid == 0) taken = ahead;
+            __syncthreads();
+            next = __builtin_amdgcn_readfirstlane(taken);
+            if (next >= total) return;
+            if (tid == 0) ahead = atomicAdd(b.p.counter, 1);
+        } else if (next >= stop) {
+            return;
+        }
+        const int r = last_base(b.n, next, [&](int i) { return b.p.requests[i].base; });
+        const Request q = b.p.requests[r];
+        const int windows = b.p.requests[r + 1].window_base - q.window_base, steps = steps_of(q.longest);
+        int64_t from, to;
+        int s0, s1, piece;
+        if (size == 1) {
+            const int64_t of_head = (b.p.requests[r + 1].base - q.base) / a.kv_heads;  // steps that its windows see
+            const int head = (int)((next - q.base) / of_head), line = (int)(next - q.base - head * of_head);
+            const int *before = b.p.window_steps + q.window_base;
+            const int w = last_base(windows, line, [&](int i) { return (int64_t)before[i]; });
+            s0 = line - before[w];
+            s1 = (int)min((int64_t)steps_of(b.p.window_max[q.window_base + w]), s0 + (stop - next));
+            from = (int64_t)head * windows + w;
+            to = from + 1;
+            piece = (int)from;
+            next += s1 - s0;
+        } else {
+            const int ranges = (steps + kRange - 1) / kRange, i = (int)(next - q.base);
+            piece = i / ranges;
+            s0 = (i - piece * ranges) * kRange;
+            s1 = min(s0 + kRange, steps);
+            from = (int64_t)piece * size;
+            to = min(from + size, (int64_t)windows * a.kv_heads);
+        }
+        const int64_t all = (int64_t)windows * a.kv_heads;
+        const int *pages = a.table + (int64_t)r * a.table_stride;
+        const auto token = [&](int s) { return s * kTile + 32 * NT * wave + NT * n; };  // this lane's first one
+        const auto page_of = [&](int s) { return pages[min((int64_t)token(min(s, s1 - 1)), cap - 1) >> a.lp]; };
+        const auto in_cache = [&](int pg) { return pg >= 0 && pg < a.n_pages; };
+        const int page = page_of(s0);
+        for (int64_t at = from; at < to; ++at) {
+            const int head = (int)(at / windows), w = (int)(at - (int64_t)head * windows);
+            const int most = b.p.window_max[q.window_base + w], least = b.p.window_min[q.window_base + w];
+            const int width = b.parts > 1 ? min(window_heads, a.per - w % b.parts * window_heads)
+                                          : min(b.rows, q.row1 - q.row0 - w * b.rows) * a.per;
+            const int cols = (width + 31) & ~31, row0 = q.row0 + (b.parts > 1 ? w / b.parts : w * b.rows);
+            const int head0 = head * a.per + (b.parts > 1 ? w % b.parts * window_heads : 0);
+            const bool sees = most > s0 * kTile && width > 0;
+            const int end = sees ? min(s1, steps_of(most)) : s0;
+            if (sees) {
+                // Queries are asked for before the wait for the window before.  This thread's: piece
+                // `part` of columns first, first + STRIDE, ..  (Their addresses go on by constants: a
+                // product of 64 bits each would cost as much as eight exponentials.)
+                constexpr int STRIDE = kBlock / PER, ROUNDS = window_of(D) / STRIDE, BATCH = 8;
+                const int first = tid / PER, part = tid % PER;
+                const auto row_of = [&](int col) { return b.parts > 1 ? 0 : (int)((u32)col * b.per_inverse >> 16); };
+                const int row1 = row_of(first);
+                int in_row = first - row1 * a.per, col = first;
+                const char *from_q = (const char *)a.q + 2 * ((row0 + row1) * a.q_row + (head0 + in_row) * a.q_head + 8 * part);
+                u32x4 x[BATCH];
+                const auto ask = [&] {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) sum[t] = 0.0f;
-
-        for (int64_t at = from; at < to;) {
-            const int head = (int)(at / chunks), c0 = (int)(at - (int64_t)head * chunks);
-            const int c1 = (int)min((int64_t)chunks, c0 + (to - at));
-            at += c1 - c0;
-            frag k[NT][D / 16];
-            float scale;
-            bool loaded = false;
-            for (int cs = c0; cs < c1; cs += 64) {
-                // the chunks that see this tile, and those whose rows all see all of it
-                const int mine = cs + lane;
-                const int most = mine < c1 ? b.p.chunk_max[first_chunk + mine] : 0;
-                const int least = mine < c1 ? b.p.chunk_min[first_chunk + mine] : 0;
-                uint64_t some = __ballot(most > tile0);
-                const uint64_t whole = __ballot(least >= tile0 + kTile);
-                if (some == 0) continue;
-                if (!loaded) {
-                    u32x4 raw[NT][D / 32];
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int j = 0; j < D / 32; ++j)
-                            raw[t][j] = *(const u32x4 *)(codes + ((int64_t)head << a.lp) * D + t * D + 32 * j);
-                    scale = scales[head] * a.scale2;
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int j = 0; j < D / 32; ++j) {
-                            k[t][2 * j] = eight<C, T>(raw[t][j][0], raw[t][j][1]);
-                            k[t][2 * j + 1] = eight<C, T>(raw[t][j][2], raw[t][j][3]);
+                    for (int i = 0; i < BATCH; ++i) {
+                        x[i] = *(const u32x4 *)(col < width ? from_q : (const char *)a.q);
+                        col += STRIDE;
+                        in_row += b.skip_heads;
+                        from_q += b.skip;
+                        if (in_row >= a.per && b.parts == 1) {
+                            in_row -= a.per;
+                            from_q += b.wrap;
                         }
-                    loaded = true;
-                }
-                u32x4 x[PIECES];
-                float lse = 0.0f;
+                    }
+                };
+                ask();
+                Softmax mine = {__builtin_inff(), 0.0f};
                 int len = 0;
-                const auto fetch = [&](int c) {
-                    int row = row0, h = head * a.per;
-                    bool on = col < (b.parts > 1 ? part_heads : b.rows * a.per);
-                    if (b.parts > 1) {
-                        row += c / b.parts;
-                        const int at = c % b.parts * part_heads + chead;
-                        on = on && at < a.per;
-                        h += at;
-                    } else {
-                        row += c * b.rows + crow;
-                        h += chead;
-                    }
-                    on = on && row < row1;
-                    lse = -__builtin_inff();
-                    len = 0;
-#pragma unroll
-                    for (int j = 0; j < PIECES; ++j) x[j] = u32x4{0, 0, 0, 0};
-                    if (!on) return;
-                    const char *q = (const char *)a.q + 2 * (row * a.q_row + h * a.q_head) + 16 * (tid & 3);
-#pragma unroll
-                    for (int j = 0; j < PIECES; ++j) x[j] = *(const u32x4 *)(q + 64 * j);
-                    lse = a.lse[(int64_t)row * a.heads + h];
-                    len = (int)min((int64_t)max(a.row_lengths[row], 0), cap);
-                };
-                const auto lay_out = [&](Chunk<D> &o) {
-                    const Softmax s = softmax_of(lse, a.stretch);
-                    // (what a row without a softmax holds is not looked at)
-#pragma unroll
-                    for (int j = 0; j < PIECES; ++j)
-                        *(u32x4 *)&o.q[col][16 * (tid & 3) + 64 * j] = s.fine == 0.0f ? u32x4{0, 0, 0, 0} : x[j];
-                    if ((tid & 3) == 0) {
-                        o.lse2[col] = s.lse2;
-                        o.fine[col] = s.fine;
-                        o.len[col] = len;
-                    }
-                };
-                int c = __builtin_ctzll(some), turn = 0;
-                fetch(cs + c);
-                __syncthreads();  // the chunk that was in the first buffer is done with
-                lay_out(buf[0]);
+                if (tid < width) {
+                    const int row = row_of(tid), h = head0 + tid - row * a.per;
+                    mine = softmax_of(a.lse[(int64_t)(row0 + row) * a.heads + h], a.stretch);
+                    len = (int)min((int64_t)max(a.row_lengths[row0 + row], 0), cap);
+                }
+                __syncthreads();  // the window before is done with
+                if (tid < window_of(D)) {
+                    o.lse2[tid] = mine.lse2;
+                    o.fine[tid] = mine.fine;
+                    o.len[tid] = len;
+                }
                 __syncthreads();
-                while (some) {
-                    const Chunk<D> &o = buf[turn];
-                    some &= some - 1;
-                    const int next = some ? __builtin_ctzll(some) : -1;
-                    if (next >= 0) fetch(cs + next);
-                    const bool masked = !(whole >> c & 1);
-                    const int left = min(kChunk, b.parts > 1 ? part_heads : min(b.rows, row1 - row0 - (cs + c) * b.rows) * a.per);
+#pragma unroll 1
+                for (int i0 = 0; i0 < ROUNDS; i0 += BATCH) {
+                    if (i0 > 0) ask();
 #pragma unroll
-                    for (int c32 = 0; c32 < kChunk; c32 += 32) {
-                        if (c32 >= left) break;
-                        f32x16 y[NT];
-#pragma unroll
-                        for (int t = 0; t < NT; ++t)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) y[t][i] = 0.0f;
-                        const uint8_t *q = o.q[c32 + n] + 32 * g;
-#pragma unroll
-                        for (int j = 0; j < D / 16; ++j) {
-                            const frag z = __builtin_bit_cast(frag, *(const u32x4 *)(q + 64 * (j >> 1) + 16 * (j & 1)));
-#pragma unroll
-                            for (int t = 0; t < NT; ++t) y[t] = Act<T>::mfma32(z, k[t][j], y[t]);
-                        }
-                        // place i of half g is column 8 (i / 4) + 4 g + i % 4
-#pragma unroll
-                        for (int i0 = 0; i0 < 16; i0 += 4) {
-                            const int at = c32 + 2 * i0 + 4 * g;
-                            const f32x4 l = *(const f32x4 *)&o.lse2[at], f = *(const f32x4 *)&o.fine[at];
-                            if (masked) {
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    const int len = o.len[at + i];
-#pragma unroll
-                                    for (int t = 0; t < NT; ++t) {
-                                        const float p = exp2_(fmaf(y[t][i0 + i], scale, -l[i])) * f[i];
-                                        sum[t] += tok + t < len ? p : 0.0f;
-                                    }
-                                }
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                                    for (int t = 0; t < NT; ++t)
-                                        sum[t] = fmaf(exp2_(fmaf(y[t][i0 + i], scale, -l[i])), f[i], sum[t]);
-                            }
-                        }
+                    for (int i = 0; i < BATCH; ++i) {
+                        const int c = first + (i0 + i) * STRIDE;
+                        // (columns past the window's; and what a row without a softmax holds is not looked at)
+                        *(u32x4 *)&o.q[c][16 * part] = o.fine[c] == 0.0f ? u32x4{0, 0, 0, 0} : x[i];
                     }
-                    if (next >= 0) lay_out(buf[turn ^ 1]);
-                    __syncthreads();
-                    turn ^= 1;
-                    c = next;
+                    if ((i0 + BATCH) * STRIDE >= cols) break;
                 }
             }
-        }
-#pragma unroll
-        for (int t = 0; t < NT; ++t) sum[t] += __shfl_xor(sum[t], 32);
-        if (g == 0) {
-            if (all <= size) {
-                float *w = a.weights + a.weight_offsets[r];
+            u32x4 raw[NT][D / 32];
+            float raw_scale;
+            const auto fetch = [&](int s, int pg) {
+                const u32 page = in_cache(pg) ? pg : 0;
+                const u32 row = page * b.page_rows + (u32)(head << a.lp) + (u32)(token(s) & ((1 << a.lp) - 1));
+                const uint8_t *p = a.k + (uint64_t)row * D + 16 * g;
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
-                    if (there && tok + t < longest) w[tok + t] += sum[t];
-            } else {
-                float *w = b.p.parts + ((int64_t)b.p.slot_base[r] + i) * kTile + 32 * NT * wave + NT * n;
 #pragma unroll
-                for (int t = 0; t < NT; ++t) w[t] = sum[t];
+                    for (int j = 0; j < D / 32; ++j) raw[t][j] = *(const u32x4 *)(p + t * D + 32 * j);
+                raw_scale = a.ks[page * a.scale_stride + head];
+            };
+            int next_page = page;
+            if (sees) {
+                fetch(s0, page);
+                next_page = page_of(s0 + 1);
+                __syncthreads();
             }
+#pragma unroll 1
+            for (int s = s0; s < end; ++s) {
+                const int base = s * kTile + 32 * NT * wave, tok = base + NT * n;
+                float sum[NT] = {0.0f, 0.0f};
+                frag k[NT][D / 16];
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int j = 0; j < D / 32; ++j) {
+                        k[t][2 * j] = eight<C, T>(raw[t][j][0], raw[t][j][1]);
+                        k[t][2 * j + 1] = eight<C, T>(raw[t][j][2], raw[t][j][3]);
+                    }
+                const float scale = raw_scale * a.scale2;
+                // the next step's codes are on their way beside the products (but for heads of 256,
+                // whose keys take half of the registers); after the last step the last ones again
+                if (D < 256) {
+                    fetch(min(s + 1, end - 1), next_page);
+                    next_page = page_of(s + 2);
+                }
+                if (base + 32 * NT <= least) pass<D, T>(o, cols, k, scale, sum);
+                else if (base < most) pass_masked<D, T>(o, cols, k, scale, sum, tok);
+                if (D == 256) {
+                    fetch(min(s + 1, end - 1), next_page);
+                    next_page = page_of(s + 2);
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) sum[t] += __shfl_xor(sum[t], 32);
+                if (g == 0) {
+                    if (all > size) {
+                        f32x2 *to = (f32x2 *)(b.p.parts + ((int64_t)q.part_base + (int64_t)piece * steps_of(q.longest) + s) * kTile +
+                                              (tok - s * kTile));
+                        f32x2 y = {sum[0], sum[1]};
+                        if (at > from) y += *to;  // (this workgroup's own, of the window before)
+                        *to = y;
+                    } else if (tok < most && in_cache(page_of(s))) {
+                        float *to = a.weights + a.weight_offsets[r] + tok;
+                        to[0] += sum[0];
+                        if (tok + 1 < most) to[1] += sum[1];
+                    }
+                }
+            }
+            // a piece of several windows begins with all of its steps
+            if (size > 1 && all > size && at == from && g == 0)
+                for (int s = end; s < s1; ++s)
+                    *(f32x2 *)(b.p.parts + ((int64_t)q.part_base + (int64_t)piece * steps_of(q.longest) + s) * kTile +
+                               (token(s) - s * kTile)) = f32x2{0.0f, 0.0f};
         }
     }
 }
 
-// Tiles whose sums lie in parts: a thread to a token.
-__global__ __launch_bounds__(kTile) void join_kernel(BlockArgs b) {
+// Steps whose sums lie in parts: 64 tokens of one to a workgroup, its parts over 16 groups of threads.
+__global__ __launch_bounds__(1024) void join_kernel(BlockArgs b) {
+    constexpr int GROUPS = 16, AHEAD = 12;
+    __shared__ float sums[GROUPS][64];
     const WeighArgs &a = b.a;
-    const int tid = threadIdx.x, total = b.p.tile_base[b.n];
-    for (int i = blockIdx.x; i < total; i += gridDim.x) {
-        const int r = last_base(b.p.tile_base, b.n, i), tile = i - b.p.tile_base[r];
-        const int tiles = b.p.tile_base[r + 1] - b.p.tile_base[r], slot = b.p.slot_base[r];
-        const int pieces = (b.p.slot_base[r + 1] - slot) / tiles, tok = tile * kTile + tid;
-        if (tok >= b.p.longest[r]) continue;
-        const int pg = a.table[(int64_t)r * a.table_stride + (tok >> a.lp)];
-        const float *parts = b.p.parts + ((int64_t)slot + tile) * kTile + tid;
-        float sum = 0.0f;
-        for (int p0 = 0; p0 < pieces; p0 += 8) {
-            float x[8];
-#pragma unroll
-            for (int p = 0; p < 8; ++p) x[p] = p0 + p < pieces ? parts[(int64_t)(p0 + p) * tiles * kTile] : 0.0f;
-#pragma unroll
-            for (int p = 0; p < 8; ++p) sum += x[p];
+    const int lane = threadIdx.x & 63, group = threadIdx.x >> 6;
+    const int total = b.p.requests[b.n].step_base, size = *b.p.size;
+    for (int64_t i = blockIdx.x; i < (int64_t)total * (kTile / 64); i += gridDim.x) {
+        const int at = (int)(i / (kTile / 64));
+        const int r = last_base(b.n, at, [&](int j) { return (int64_t)b.p.requests[j].step_base; });
+        const Request q = b.p.requests[r], next = b.p.requests[r + 1];
+        const int step = at - q.step_base, steps = next.step_base - q.step_base, windows = next.window_base - q.window_base;
+        const int pieces = (next.part_base - q.part_base) / steps, in = (int)(i % (kTile / 64)) * 64 + lane;
+        const int tok = step * kTile + in;
+        const float *parts = b.p.parts + ((int64_t)q.part_base + step) * kTile + in;
+        float sum = 0.0f, old = 0.0f, *to = nullptr;
+        if (group == 0 && tok < q.longest) {
+            const int pg = a.table[(int64_t)r * a.table_stride + (tok >> a.lp)];
+            to = a.weights + a.weight_offsets[r] + tok;
+            old = *to;
+            if (pg < 0 || pg >= a.n_pages) to = nullptr;
         }
-        if (pg >= 0 && pg < a.n_pages) a.weights[a.weight_offsets[r] + tok] += sum;
+        for (int p0 = group; p0 < pieces; p0 += AHEAD * GROUPS) {
+            float x[AHEAD];
+            int most[AHEAD];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                const int p = min(p0 + j * GROUPS, pieces - 1);
+                x[j] = parts[(int64_t)p * steps * kTile];
+                most[j] = b.p.window_max[q.window_base + p % windows];
+            }
+            // (a piece of one window has no parts of steps that it does not see: what lies there is anything)
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j)
+                sum += p0 + j * GROUPS < pieces && (size > 1 || most[j] > step * kTile) ? x[j] : 0.0f;
+        }
+        sums[group][lane] = sum;
+        __syncthreads();
+        if (to) {
+#pragma unroll
+            for (int j = 1; j < GROUPS; ++j) sum += sums[j][lane];
+            *to = old + sum;
+        }
+        __syncthreads();
     }
 }
 
-// A call's division into chunks, and the workspace's.
+// A call's division into windows, and the workspace's.
 struct Sizes {
-    int rows, parts, max_chunks;
+    int rows, parts;
+    int64_t max_windows;
     size_t bytes;
 };
-Sizes sizes_of(int64_t n_rows, int64_t n_requests, int per) {
+Sizes sizes_of(int64_t n_rows, int64_t n_requests, int per, int cols) {
     Sizes s;
-    s.parts = (per + kChunk - 1) / kChunk;
-    s.rows = s.parts > 1 ? 1 : kChunk / per;
-    const int64_t chunks = s.parts > 1 ? n_rows * s.parts : n_rows / s.rows + n_requests;
-    s.max_chunks = (int)(chunks < 0x7FFFFFF0 ? chunks : 0x7FFFFFF0);
-    s.bytes = 256 + 8 * (size_t)(n_requests + 1) + 4 * (4 * (size_t)(n_requests + 1) + 2 * (size_t)chunks) + 256 +
-              (size_t)2 * kUnits * kTile * sizeof(float);
+    s.parts = (per + cols - 1) / cols;
+    s.rows = s.parts > 1 ? 1 : cols / per;
+    s.max_windows = s.parts > 1 ? n_rows * s.parts : n_rows / s.rows + n_requests;
+    s.bytes = 256 + sizeof(Request) * (size_t)(n_requests + 1) + 12 * (size_t)s.max_windows +
+              (size_t)kParts * kTile * sizeof(float);
     return s;
 }
 
@@ -589,7 +879,8 @@ extern "C" size_t serve_weigh_workspace(int32_t n_rows, int32_t n_requests, int3
     using namespace paged;
     if (n_rows < 0 || n_requests < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0) return 0;
     if (device_cus() == 0) return 0;
-    return many(n_rows, n_requests) ? sizes_of(n_rows, n_requests, heads / kv_heads).bytes : 256;
+    // (the smaller windows of heads of 256 are more)
+    return many(n_rows, n_requests) ? sizes_of(n_rows, n_requests, heads / kv_heads, window_of(256)).bytes : 256;
 }
 
 extern "C" int serve_weigh(const paged_kv_cache *cache, int32_t act, const void *q, int64_t q_row, int64_t q_head,
@@ -624,31 +915,34 @@ extern "C" int serve_weigh(const paged_kv_cache *cache, int32_t act, const void 
     const bool block = many(n_rows, n_requests);
     dim3 grid;
     if (block) {
-        const Sizes s = sizes_of(n_rows, n_requests, b.a.per);
-        if (s.max_chunks == 0x7FFFFFF0) return PAGED_KV_EUNSUPPORTED;
+        const Sizes s = sizes_of(n_rows, n_requests, b.a.per, window_of(cache->head_dim));
+        if (s.max_windows > 0x7FFFFFF0) return PAGED_KV_EUNSUPPORTED;
         b.n = n_requests;
         b.rows = s.rows;
         b.parts = s.parts;
-        b.max_chunks = s.max_chunks;
+        b.max_windows = (int)s.max_windows;
+        b.page_rows = (u32)(cache->page_stride / cache->head_dim);
+        b.per_inverse = 65536u / b.a.per + 1;
+        const int stride = kBlock / (cache->head_dim / 8), rows = s.parts > 1 ? 0 : stride / b.a.per;
+        b.skip_heads = stride - rows * b.a.per;
+        b.skip = 2 * (rows * q_row + b.skip_heads * q_head);
+        b.wrap = 2 * (q_row - b.a.per * q_head);
         char *at = (char *)workspace;
         const auto take = [&](size_t bytes) {
             char *p = at;
             at += bytes;
             return p;
         };
-        b.p.parts = (float *)take((size_t)2 * kUnits * kTile * sizeof(float));
+        b.p.parts = (float *)take((size_t)kParts * kTile * sizeof(float));
         b.p.counter = (int *)take(128);
         b.p.size = (int *)take(128);
-        b.p.unit_base = (int64_t *)take(8 * (size_t)(n_requests + 1));
-        b.p.slot_base = (int *)take(4 * (size_t)(n_requests + 1));
-        b.p.tile_base = (int *)take(4 * (size_t)(n_requests + 1));
-        b.p.chunk_base = (int *)take(4 * (size_t)(n_requests + 1));
-        b.p.longest = (int *)take(4 * (size_t)(n_requests + 1));
-        b.p.chunk_max = (int *)take(4 * (size_t)s.max_chunks);
-        b.p.chunk_min = (int *)take(4 * (size_t)s.max_chunks);
+        b.p.requests = (Request *)take(sizeof(Request) * (size_t)(n_requests + 1));
+        b.p.window_max = (int *)take(4 * (size_t)s.max_windows);
+        b.p.window_min = (int *)take(4 * (size_t)s.max_windows);
+        b.p.window_steps = (int *)take(4 * (size_t)s.max_windows);
         rc = launch(plan_kernel, dim3(1), dim3(kPlan), stream, b);
         if (rc != PAGED_KV_OK) return rc;
-        grid = dim3((unsigned)(device_cus() * (cache->head_dim == 256 ? 2 : 3)));
+        grid = dim3((unsigned)(device_cus() * 2));
     } else {
         while (b.a.steps < 4 && cap / (2 * b.a.steps * kTile) * n_requests >= 1024) b.a.steps *= 2;
         const int64_t tokens = (int64_t)kTile * b.a.steps;
@@ -658,6 +952,6 @@ extern "C" int serve_weigh(const paged_kv_cache *cache, int32_t act, const void 
     rc = cache->head_dim == 64    ? launch_dim<64>(b, act, cache->code, l, stream)
          : cache->head_dim == 128 ? launch_dim<128>(b, act, cache->code, l, stream)
                                   : launch_dim<256>(b, act, cache->code, l, stream);
-    if (rc == PAGED_KV_OK && block) rc = launch(join_kernel, dim3(256), dim3(kTile), stream, b);
+    if (rc == PAGED_KV_OK && block) rc = launch(join_kernel, dim3(512), dim3(1024), stream, b);
     return rc;
 }

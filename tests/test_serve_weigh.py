@@ -218,6 +218,43 @@ def test_repeats_to_the_bit_captured_and_on_other_streams():
             assert torch.equal(w, ref), i
 
 
+def test_more_parts_than_the_workspace_holds():
+    """Windows add up in one part then; beside them a request of one window, one without rows and one whose windows
+    are a single piece."""
+    from paper_2609_08450_amd import evict
+
+    # (one head is compared at a time: the others have an lse of -inf but for the first and the last)
+    s = Setup([20000, 900, 50, 700], [1280, 3, 0, 40], page=256, kv=8, heads=128, dim=64, values=False).cuda()
+    steps = sum(-(-L // 256) * -(-n * 16 // 256) * 8 for L, n in zip(s.lens, (1280, 3, 0, 40)))
+    assert steps > 49152
+    lse, total, bound = torch.full((s.n_rows, 128), -math.inf, device="cuda"), {}, {}
+    for r in (0, 1, 3):
+        a, b, L = int(s.row_starts[r]), int(s.row_starts[r + 1]), s.lens[r]
+        k, there = s.tokens("k", r, L)
+        assert bool(there.all())
+        seen = torch.arange(L, device="cuda") < s.row_lengths[a:b, None]
+        for h in (0, 77, 127):
+            q = s.q[a:b, h].double()
+            x = s.scale * torch.matmul(q, k[h // 16].t())
+            x.masked_fill_(~seen, -math.inf)
+            lse[a:b, h] = torch.logsumexp(x, 1).float()
+            z = lse[a:b, h, None].double()
+            p = torch.exp(x - z)
+            size = s.scale * torch.matmul(q.abs(), k[h // 16].abs().t())
+            total[r] = total.get(r, 0) + p.sum(0)
+            x.masked_fill_(~seen, 0.0)
+            bound[r] = bound.get(r, 0) + (p * (64 * 2.0 ** -24 * size + 2.0 ** -22 * (x.abs() + z.abs()) + 2.0 ** -21)).sum(0)
+    w = torch.zeros((4, 20000), device="cuda")
+    for i in range(2):
+        evict.weigh(s.cache(), s.q, lse, s.table, s.row_starts, s.row_lengths, s.scale, w, torch.arange(4).cuda() * 20000)
+    torch.cuda.synchronize()
+    for r in (0, 1, 3):
+        L = s.lens[r]
+        off = (w[r, :L].double() - 2 * total[r]).abs() - 2 * bound[r] - (s.n_rows * 128 + 1) * 2.0 ** -23 * total[r]
+        assert bool((off <= 0).all()) and not bool(w[r, L:].any()), r
+    assert not bool(w[2].any())
+
+
 def test_far_offsets():
     """Weights past 2^31 elements, and codes past 2^32 bytes."""
     from paper_2609_08450_amd import evict, paged
