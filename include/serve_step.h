@@ -67,8 +67,8 @@ int serve_rotate(int32_t act, const serve_rotary *rotary, const void *positions,
 
 /* Bytes of workspace for serve_weigh on the current device, for any lengths; 0
  * for arguments that it refuses.  256-byte aligned; it needs no preparation; calls
- * that overlap do not share one.  Calls of at most one row to a request
- * (n_rows <= n_requests) use none: it may be NULL, of any size. */
+ * that overlap do not share one.  Where it is 256 a call uses none, and it may be
+ * NULL: n_rows up to n_requests, or to 256 / heads. */
 size_t serve_weigh_workspace(int32_t n_rows, int32_t n_requests, int32_t heads, int32_t kv_heads);
 
 /* weights[weight_offsets[r] + j] += sum_i sum_h exp(scale q[i][h] . k_j - lse[i][h])

@@ -29,6 +29,8 @@ struct WeighArgs {
     int table_stride, table_width;
     const int *row_starts, *row_lengths;
     int n_rows, steps;
+    int64_t limit;   // rows x heads of the requests that the kernel of few rows takes
+    u32 page_rows;   // rows of head_dim codes from one page to the next
     float scale2, stretch;  // scale * log2(e), and what its rounding leaves of it: (1 + stretch) scale2
     float *weights;
     const int64_t *weight_offsets;
@@ -67,6 +69,7 @@ __global__ __launch_bounds__(kBlock) void weigh_rows_kernel(WeighArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, g = lane >> 5;
     const int r = blockIdx.y;
     const int row0 = min(max(a.row_starts[r], 0), a.n_rows), row1 = min(max(a.row_starts[r + 1], row0), a.n_rows);
+    if ((int64_t)(row1 - row0) * a.heads > a.limit) return;
     const int64_t cap = (int64_t)a.table_width << a.lp;
     int longest = 0, shortest = 0x7FFFFFFF;
     for (int i = row0 + lane; i < row1; i += 64) {
@@ -224,7 +227,6 @@ struct BlockArgs {
     WeighArgs a;
     int n, rows, parts;  // requests; rows of a window; windows of a row, where a head's queries are more than a window
     int max_windows;
-    u32 page_rows;    // rows of head_dim codes from one page to the next
     u32 per_inverse;  // 65536 / per, rounded up: a column's row without a division
     int skip_heads;   // from one column of a thread to its next: heads (of the row it comes to),
     int64_t skip, wrap;  // bytes of q, and bytes more where the head is past the row's last
@@ -285,7 +287,10 @@ __global__ __launch_bounds__(kPlan) void plan_kernel(BlockArgs b) {
             row0 = bounded(a, r);
             row1 = max(bounded(a, r + 1), row0);
         }
-        const int64_t mine = b.parts > 1 ? (int64_t)(row1 - row0) * b.parts : (row1 - row0 + b.rows - 1) / b.rows;
+        // (the kernel of few rows has taken the others)
+        const int64_t mine = (int64_t)(row1 - row0) * a.heads <= a.limit ? 0
+                             : b.parts > 1 ? (int64_t)(row1 - row0) * b.parts
+                                           : (row1 - row0 + b.rows - 1) / b.rows;
         const int from = (int)min(windows + prefix(mine, waves, &all), (int64_t)b.max_windows);
         first[tid] = from;
         most_of[tid] = 0;
@@ -724,7 +729,7 @@ __global__ __launch_bounds__(kBlock, 2) void weigh_block_kernel(BlockArgs b) {
             float raw_scale;
             const auto fetch = [&](int s, int pg) {
                 const u32 page = in_cache(pg) ? pg : 0;
-                const u32 row = page * b.page_rows + (u32)(head << a.lp) + (u32)(token(s) & ((1 << a.lp) - 1));
+                const u32 row = page * a.page_rows + (u32)(head << a.lp) + (u32)(token(s) & ((1 << a.lp) - 1));
                 const uint8_t *p = a.k + (uint64_t)row * D + 16 * g;
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
@@ -851,26 +856,33 @@ Sizes sizes_of(int64_t n_rows, int64_t n_requests, int per, int cols) {
     return s;
 }
 
-struct Launch {
-    bool block;
-    dim3 grid;
-};
+// Requests of up to so many rows x heads read the cache by themselves, without queries in windows (64 of 16384
+// tokens, 16 heads: 8 rows each 96 us, and 180 in windows; 16 rows 169 and 203; one of 131072 tokens, 32 heads:
+// 8 rows 40 and 52, 16 rows 66 and 57).
+constexpr int kFew = 256;
+
+// Whether a call may have others.  (Where rows are no more than requests, as single tokens are, none is looked
+// for: the plan would cost as much as a short call.)
+inline bool many(int n_rows, int n_requests, int heads) { return n_rows > n_requests && (int64_t)n_rows * heads > kFew; }
 
 template <int D, class T, class C>
-int launch_types(const BlockArgs &b, Launch l, void *stream) {
-    return l.block ? launch(weigh_block_kernel<D, T, C>, l.grid, dim3(kBlock), stream, b)
-                   : launch(weigh_rows_kernel<D, T, C>, l.grid, dim3(kBlock), stream, b.a);
+int launch_types(BlockArgs &b, bool block, int n_requests, void *stream) {
+    WeighArgs &a = b.a;
+    const int64_t cap = (int64_t)a.table_width << a.lp;
+    while (a.steps < 4 && cap / (2 * a.steps * kTile) * n_requests >= 1024) a.steps *= 2;
+    const int64_t tokens = (int64_t)kTile * a.steps;
+    const int rc = launch(weigh_rows_kernel<D, T, C>, dim3((unsigned)((cap + tokens - 1) / tokens), (unsigned)n_requests),
+                          dim3(kBlock), stream, a);
+    if (rc != PAGED_KV_OK || !block) return rc;
+    return launch(weigh_block_kernel<D, T, C>, dim3((unsigned)device_cus() * 2), dim3(kBlock), stream, b);
 }
 
 template <int D>
-int launch_dim(const BlockArgs &b, int act, int code, Launch l, void *stream) {
+int launch_dim(BlockArgs &b, int act, int code, bool block, int n, void *stream) {
     if (code == PAGED_KV_E4M3)
-        return act == PAGED_KV_BF16 ? launch_types<D, bf16, E4M3>(b, l, stream) : launch_types<D, f16, E4M3>(b, l, stream);
-    return act == PAGED_KV_BF16 ? launch_types<D, bf16, Int8>(b, l, stream) : launch_types<D, f16, Int8>(b, l, stream);
+        return act == PAGED_KV_BF16 ? launch_types<D, bf16, E4M3>(b, block, n, stream) : launch_types<D, f16, E4M3>(b, block, n, stream);
+    return act == PAGED_KV_BF16 ? launch_types<D, bf16, Int8>(b, block, n, stream) : launch_types<D, f16, Int8>(b, block, n, stream);
 }
-
-// More rows than requests: rows share their keys.
-inline bool many(int n_rows, int n_requests) { return n_rows > n_requests; }
 
 }  // namespace
 }  // namespace paged
@@ -880,7 +892,7 @@ extern "C" size_t serve_weigh_workspace(int32_t n_rows, int32_t n_requests, int3
     if (n_rows < 0 || n_requests < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0) return 0;
     if (device_cus() == 0) return 0;
     // (the smaller windows of heads of 256 are more)
-    return many(n_rows, n_requests) ? sizes_of(n_rows, n_requests, heads / kv_heads, window_of(256)).bytes : 256;
+    return many(n_rows, n_requests, heads) ? sizes_of(n_rows, n_requests, heads / kv_heads, window_of(256)).bytes : 256;
 }
 
 extern "C" int serve_weigh(const paged_kv_cache *cache, int32_t act, const void *q, int64_t q_row, int64_t q_head,
@@ -896,24 +908,23 @@ extern "C" int serve_weigh(const paged_kv_cache *cache, int32_t act, const void 
         scale - scale != 0.0f)
         return PAGED_KV_EINVAL;
     if (n_rows == 0 || n_requests == 0) return PAGED_KV_OK;
+    const bool block = many(n_rows, n_requests, heads);
     if (!q || !lse || !table || !row_starts || !row_lengths || !weights || !weight_offsets || !aligned16(q) ||
-        q_row % 8 || q_head % 8 || (many(n_rows, n_requests) && !workspace) || (uintptr_t)workspace % 256)
+        q_row % 8 || q_head % 8 || (block && !workspace) || (uintptr_t)workspace % 256)
         return PAGED_KV_EINVAL;
     const int lp = log2_page(cache->page);
     if (((int64_t)table_width << lp) > 0x7FFFFFFF - 65536 || n_requests > 65535) return PAGED_KV_EUNSUPPORTED;
     const size_t need = serve_weigh_workspace(n_rows, n_requests, heads, cache->n_heads);
     if (need == 0) return PAGED_KV_EUNSUPPORTED;
-    if (many(n_rows, n_requests) && workspace_bytes < need) return PAGED_KV_EWORKSPACE;
+    if (block && workspace_bytes < need) return PAGED_KV_EWORKSPACE;
     const double exact = (double)scale * 1.4426950408889634;
     const float scale2 = (float)exact;
     BlockArgs b = {};
     b.a = {(const uint8_t *)cache->k, cache->k_scale, cache->page_stride, cache->scale_stride, cache->n_pages,
            lp, cache->n_heads, q, q_row, q_head, heads, heads / cache->n_heads, lse, table, table_stride,
-           table_width, row_starts, row_lengths, n_rows, 1, scale2, scale2 > 0.0f ? (float)(exact / scale2 - 1.0) : 0.0f,
+           table_width, row_starts, row_lengths, n_rows, 1, block ? kFew : INT64_MAX,
+           (u32)(cache->page_stride / cache->head_dim), scale2, scale2 > 0.0f ? (float)(exact / scale2 - 1.0) : 0.0f,
            weights, weight_offsets};
-    const int64_t cap = (int64_t)table_width << lp;
-    const bool block = many(n_rows, n_requests);
-    dim3 grid;
     if (block) {
         const Sizes s = sizes_of(n_rows, n_requests, b.a.per, window_of(cache->head_dim));
         if (s.max_windows > 0x7FFFFFF0) return PAGED_KV_EUNSUPPORTED;
@@ -921,7 +932,6 @@ extern "C" int serve_weigh(const paged_kv_cache *cache, int32_t act, const void 
         b.rows = s.rows;
         b.parts = s.parts;
         b.max_windows = (int)s.max_windows;
-        b.page_rows = (u32)(cache->page_stride / cache->head_dim);
         b.per_inverse = 65536u / b.a.per + 1;
         const int stride = kBlock / (cache->head_dim / 8), rows = s.parts > 1 ? 0 : stride / b.a.per;
         b.skip_heads = stride - rows * b.a.per;
@@ -942,16 +952,10 @@ extern "C" int serve_weigh(const paged_kv_cache *cache, int32_t act, const void 
         b.p.window_steps = (int *)take(4 * (size_t)s.max_windows);
         rc = launch(plan_kernel, dim3(1), dim3(kPlan), stream, b);
         if (rc != PAGED_KV_OK) return rc;
-        grid = dim3((unsigned)(device_cus() * 2));
-    } else {
-        while (b.a.steps < 4 && cap / (2 * b.a.steps * kTile) * n_requests >= 1024) b.a.steps *= 2;
-        const int64_t tokens = (int64_t)kTile * b.a.steps;
-        grid = dim3((unsigned)((cap + tokens - 1) / tokens), (unsigned)n_requests);
     }
-    const Launch l = {block, grid};
-    rc = cache->head_dim == 64    ? launch_dim<64>(b, act, cache->code, l, stream)
-         : cache->head_dim == 128 ? launch_dim<128>(b, act, cache->code, l, stream)
-                                  : launch_dim<256>(b, act, cache->code, l, stream);
+    rc = cache->head_dim == 64    ? launch_dim<64>(b, act, cache->code, block, n_requests, stream)
+         : cache->head_dim == 128 ? launch_dim<128>(b, act, cache->code, block, n_requests, stream)
+                                  : launch_dim<256>(b, act, cache->code, block, n_requests, stream);
     if (rc == PAGED_KV_OK && block) rc = launch(join_kernel, dim3(512), dim3(1024), stream, b);
     return rc;
 }

@@ -26,6 +26,7 @@ from . import topk as _topk
 PagedError = _paged.PagedError
 
 
+NO_WORKSPACE = 256  # bytes that stand for none
 _sizes = {}  # bytes by (rows, requests, heads, cache heads)
 
 
@@ -47,7 +48,7 @@ def weigh(cache, q, lse, table, row_starts, row_lengths, scale: float, weights, 
     """Forwards to serve_weigh(): adds to each request's weights (any contiguous float32 tensor, request r's
     from weight_offsets[r] on) what its tokens got of the attention of q [rows, heads, dim], whose ``lse``
     float32 [rows, heads] ``paged.attend`` gave.  ``workspace``: uint8 of ``workspace_size`` bytes, for a
-    program that keeps one; calls of at most one row to a request use none."""
+    program that keeps one; where that is 256 (single tokens, few rows) a call uses none."""
     dev = cache._on_current()
     qp, q_row, q_head = _paged._rows3(q, None, cache.head_dim, "q", dev)
     rows, heads, _ = q.shape
@@ -62,8 +63,9 @@ def weigh(cache, q, lse, table, row_starts, row_lengths, scale: float, weights, 
         wp, size = workspace.data_ptr(), workspace.numel()
     elif rows > n:
         size = workspace_size(cache, rows, n, heads)
-        workspace = _serve.empty(size, q, torch.uint8, stream)
-        wp = workspace.data_ptr()
+        if size > NO_WORKSPACE:
+            workspace = _serve.empty(size, q, torch.uint8, stream)
+            wp = workspace.data_ptr()
     _serve.check((_serve._lib or _serve.lib()).serve_weigh(
         cache._ref, _paged.ACTS[q.dtype], qp, q_row, q_head, heads,
         _serve.flat(lse, torch.float32, (rows, heads), "lse", dev), at, stride, width,

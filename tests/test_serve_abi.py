@@ -101,7 +101,7 @@ NO_KERNEL = [dict(page=8), dict(page=48), dict(page=512), dict(head_dim=96, page
              dict(n_pages=2 ** 31 - 1, page_stride=64 * 2048)]
 
 
-def weigh(serve, c=None, act=0, q=P, q_row=256, q_head=64, heads=4, lse=P, table=P, stride=8, width=8, starts=P, n=3, lens=P,
+def weigh(serve, c=None, act=0, q=P, q_row=256, q_head=64, heads=104, lse=P, table=P, stride=8, width=8, starts=P, n=3, lens=P,
           rows=5, scale=0.1, w=P, offsets=P, ws=P, size=1 << 40):
     return serve.lib().serve_weigh(c or cache_of(), act, q, q_row, q_head, heads, lse, table, stride, width, starts, n, lens,
                                    rows, scale, w, offsets, ws, size, None)
@@ -123,7 +123,7 @@ def test_caches_are_checked(serve):
 
 def test_weigh_refusals(serve):
     for bad in (dict(act=2), dict(act=-1), dict(q=None), dict(q=4100), dict(q_row=250), dict(q_head=4), dict(heads=0),
-                dict(heads=3), dict(lse=None), dict(table=None), dict(width=0), dict(stride=7), dict(starts=None),
+                dict(heads=103), dict(lse=None), dict(table=None), dict(width=0), dict(stride=7), dict(starts=None),
                 dict(lens=None), dict(rows=-1), dict(n=-1), dict(scale=-0.1), dict(scale=float("nan")),
                 dict(scale=float("inf")), dict(w=None), dict(offsets=None), dict(ws=None), dict(ws=4104)):
         assert weigh(serve, **bad) == EINVAL, bad

@@ -218,6 +218,15 @@ def test_repeats_to_the_bit_captured_and_on_other_streams():
             assert torch.equal(w, ref), i
 
 
+def test_requests_of_few_and_of_many_rows_in_one_call():
+    """Each kind is a kernel's own: single rows, rows x heads of 256 and of 264, a prompt, none."""
+    s = Setup([900, 300, 513, 1400, 40, 77], [1, 32, 33, 500, 0, 2], page=32, kv=2, heads=8, dim=64, values=False).cuda()
+    assert check(s) == sum(s.lens) - 40
+    # in all no more rows than requests: one request has all of them
+    s = Setup([600] + [20] * 63, [60] + [0] * 63, page=16, kv=1, heads=8, dim=128, values=False).cuda()
+    assert check(s) == 600
+
+
 def test_more_parts_than_the_workspace_holds():
     """Windows add up in one part then; beside them a request of one window, one without rows and one whose windows
     are a single piece."""
