@@ -81,7 +81,7 @@ size_t serve_weigh_workspace(int32_t n_rows, int32_t n_requests, int32_t heads, 
  *   q, act, table, row_starts, row_lengths, scale  as in paged_kv_attend; the cache
  *                   need not have values;
  *   lse             FP32 [n_rows][heads];
- *   weight_offsets  int64 [n_requests], in elements. */
+ *   weight_offsets  int64 [n_requests], in elements; no two requests' weights overlap. */
 int serve_weigh(const paged_kv_cache *cache, int32_t act, const void *q, int64_t q_row,
                 int64_t q_head, int32_t heads, const float *lse, const int32_t *table,
                 int32_t table_stride, int32_t table_width, const int32_t *row_starts,
@@ -95,7 +95,7 @@ int serve_weigh(const paged_kv_cache *cache, int32_t act, const void *q, int64_t
  * token given twice stays once).
  *   kept    int32 [n_requests][width] out: their numbers, ascending, then -1;
  *           width >= first + K + last;
- *   counts  int32 [n_requests] out;
+ *   counts  int32 [n_requests] out; neither lens nor, as kept, idx itself;
  *   weights FP32 or NULL: the weight of the i-th kept token moves to
  *           weights[weight_offsets[r] + i], and 0 follows up to lens[r].
  * lens[r] up to 2^31 - 1; one that is not positive keeps nothing. */
@@ -105,7 +105,7 @@ int serve_keep(const int32_t *idx, int32_t K, int32_t base, const int32_t *lens,
 
 /* Token i of request r becomes what its token kept[r][i] was, for i < counts[r], in the
  * pages that the request has.  kept rises (serve_keep's list), and a page belongs
- * to one request.  A page none of whose tokens moves stays as it is.  Of any other,
+ * to one request, which has it once.  A page none of whose tokens moves stays as it is.  Of any other,
  * each head gets the scale that paged_kv_store would give these values, and codes
  * code * old scale / new scale, rounded once to nearest even (int8; e4m3: by way of
  * FP32).  Codes past the last token, and pages past it, stay.  Tokens from a page
@@ -142,7 +142,7 @@ typedef struct serve_lists {
  *   of a token that the mask does not allow: -inf, whatever x is.
  *   act         PAGED_KV_BF16, PAGED_KV_F16 or SERVE_F32;
  *   logits      [n_rows][vocab], x_row elements from row to row;
- *   out         FP32 [n_rows][vocab], out_row elements from row to row; may be
+ *   out         FP32 [n_rows][vocab], out_row >= vocab elements from row to row; may be
  *               logits where these are FP32 and have its stride, or memory apart. */
 int serve_adjust(int32_t act, const void *logits, int64_t x_row, float *out, int64_t out_row,
                  int32_t n_rows, int32_t vocab, const serve_lists *lists, void *stream);

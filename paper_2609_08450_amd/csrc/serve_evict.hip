@@ -411,7 +411,8 @@ extern "C" int serve_keep(const int32_t *idx, int32_t K, int32_t base, const int
     if (K < 0 || base < 0 || n_requests < 0 || first < 0 || last < 0 || width < (int64_t)first + K + last)
         return PAGED_KV_EINVAL;
     if (n_requests == 0) return PAGED_KV_OK;
-    if ((K > 0 && !idx) || !lens || (width > 0 && !kept) || !counts || (weights && !weight_offsets) || lens == counts)
+    if ((K > 0 && !idx) || !lens || (width > 0 && !kept) || !counts || (weights && !weight_offsets) || lens == counts ||
+        (K > 0 && idx == kept))
         return PAGED_KV_EINVAL;
     if (device_cus() == 0) return PAGED_KV_EUNSUPPORTED;
     const KeepArgs a = {idx, K, base, lens, first, last, kept, width, counts, weights, weight_offsets};

@@ -191,6 +191,7 @@ extern "C" int serve_adjust(int32_t act, const void *logits, int64_t x_row, floa
     const int size = act == SERVE_F32 ? 4 : 2;
     if (!logits || !out || (uintptr_t)logits % size || (uintptr_t)out % 4) return PAGED_KV_EINVAL;
     if ((const void *)out == logits && (act != SERVE_F32 || x_row != out_row)) return PAGED_KV_EINVAL;
+    if (n_rows > 1 && out_row < vocab) return PAGED_KV_EINVAL;
     const serve_lists &l = *lists;
     if (l.tokens && !l.token_starts) return PAGED_KV_EINVAL;
     if (l.bias_ids && (!l.bias || !l.bias_starts)) return PAGED_KV_EINVAL;

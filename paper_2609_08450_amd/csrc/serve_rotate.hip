@@ -199,6 +199,8 @@ extern "C" int serve_rotate(int32_t act, const serve_rotary *rotary, const void 
     for (const serve_heads *h : both) {
         if (!h) continue;
         if (!h->in || !h->out || (uintptr_t)h->in % size || (uintptr_t)h->out % size) return PAGED_KV_EINVAL;
+        if (h->in == h->out && ((n_rows > 1 && h->in_row != h->out_row) || (h->heads > 1 && h->in_head != h->out_head)))
+            return PAGED_KV_EINVAL;
         any |= (uint64_t)h->in_row | (uint64_t)h->in_head | (uint64_t)h->out_row | (uint64_t)h->out_head |
                (uintptr_t)h->in / size | (uintptr_t)h->out / size;
     }

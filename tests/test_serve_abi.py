@@ -77,7 +77,8 @@ def test_rotate_refusals(serve):
                 dict(magnitude=float("inf")), dict(rot=0), dict(rot=31), dict(rot=66), dict(start=-1), dict(start=33),
                 dict(positions=None), dict(positions=4098), dict(positions=4100, wide=1), dict(rows=-1), dict(dim=0),
                 dict(q=dict(heads=0)), dict(k=dict(heads=0)), dict(q=dict(in_=None)), dict(q=dict(out=None)),
-                dict(q=dict(in_=4097)), dict(k=dict(out=4097)), dict(act=2, q=dict(in_=4098))):
+                dict(q=dict(in_=4097)), dict(k=dict(out=4097)), dict(act=2, q=dict(in_=4098)),
+                dict(q=dict(out_row=512)), dict(k=dict(out_head=32)), dict(rows=1, q=dict(out_head=128))):
         assert rotate(serve, **bad) == EINVAL, bad
     for bad in (dict(rot=1026, dim=2048), dict(dim=65537), dict(q=dict(heads=2 ** 30)), dict(k=dict(heads=2 ** 30))):
         assert rotate(serve, **bad) == EUNSUPPORTED, bad
@@ -134,13 +135,13 @@ def test_weigh_refusals(serve):
         assert L.serve_weigh_workspace(*sizes) == 0
 
 
-def keep(serve, idx=P, K=5, base=0, lens=P, n=3, first=1, last=2, kept=P, width=8, counts=8192, w=None, offsets=None):
+def keep(serve, idx=P, K=5, base=0, lens=P, n=3, first=1, last=2, kept=12288, width=8, counts=8192, w=None, offsets=None):
     return serve.lib().serve_keep(idx, K, base, lens, n, first, last, kept, width, counts, w, offsets, None)
 
 
 def test_keep_and_compact_refusals(serve):
     for bad in (dict(idx=None), dict(K=-1), dict(base=-1), dict(lens=None), dict(n=-1), dict(first=-1), dict(last=-1),
-                dict(kept=None), dict(width=7), dict(counts=None), dict(w=P), dict(counts=P),
+                dict(kept=None), dict(width=7), dict(counts=None), dict(w=P), dict(counts=P), dict(kept=P),
                 dict(first=2 ** 31 - 1, last=2 ** 31 - 1, width=2 ** 31 - 1)):
         assert keep(serve, **bad) == EINVAL, bad
     assert keep(serve, n=0, idx=None, lens=None) == 0
@@ -160,12 +161,12 @@ def adjust(serve, act=0, x=P, x_row=64, out=8192, out_row=64, rows=3, vocab=50, 
 
 def test_adjust_refusals(serve):
     for bad in (dict(act=3), dict(act=-1), dict(x=None), dict(x=4097), dict(act=2, x=4098), dict(out=None), dict(out=8194),
-                dict(rows=-1), dict(vocab=0), dict(x=8192), dict(act=2, x=8192, x_row=60), dict(tokens=P),
+                dict(rows=-1), dict(vocab=0), dict(x=8192), dict(act=2, x=8192, x_row=60), dict(out_row=49), dict(tokens=P),
                 dict(bias_ids=P), dict(bias_ids=P, bias=P), dict(bias_ids=P, bias_starts=P),
                 dict(mask=P, mask_stride=1, n_masks=3), dict(mask=P, mask_stride=2, n_masks=-1, row_mask=P),
                 dict(mask=P, mask_stride=2, n_masks=2)):
         assert adjust(serve, **bad) == EINVAL, bad
-    for bad in (dict(rows=65536), dict(vocab=2 ** 31 - 1)):
+    for bad in (dict(rows=65536), dict(vocab=2 ** 31 - 1, out_row=2 ** 31)):
         assert adjust(serve, **bad) == EUNSUPPORTED, bad
     assert adjust(serve, rows=0, x=None) == 0
     assert serve.lib().serve_adjust(0, P, 64, P, 64, 3, 50, None, None) == EINVAL
