@@ -96,6 +96,29 @@ def test_parts(history, biases, masks):
     Case(6, 5000, torch.bfloat16, history, biases, masks).check()
 
 
+@pytest.mark.parametrize("rows,vocab,biases", [(3, 4097, 9000), (600, 130, 400), (2, 5000, 760)])
+@pytest.mark.parametrize("act", [torch.float16, torch.float32], ids=str)
+def test_more_biases_than_a_list_holds(rows, vocab, biases, act):
+    """In chunks of both sizes, tokens that are biased many times among them."""
+    c = Case(rows, vocab, act, 20, biases, 1, special=True)
+    c.check()
+    if act is torch.float32:
+        ref = c.ref()
+        c.out = c.x
+        c.out_wide = c.x
+        from paper_2609_08450_amd import logits
+
+        assert same(logits.adjust(c.x, c.x, **c.how), ref)
+
+
+def test_as_many_biases_as_a_list_holds():
+    c = Case(3, 1000, biases=1, history=9)
+    c.biases = [[((7 * i) % 1000, float(i)) for i in range(n)] for n in (255, 256, 257)]
+    c.how["bias_ids"], c.how["bias_starts"] = ragged([[i for i, _ in b] for b in c.biases], torch.int32)
+    c.how["bias"] = ragged([[v for _, v in b] for b in c.biases], torch.float32)[0]
+    c.check()
+
+
 def test_special_values():
     """Infinities and zeros of both signs, and NaN: only in tokens that the mask allows does one stay."""
     c = Case(6, 3000, special=True)
