@@ -60,12 +60,14 @@ struct Columns {
     alignas(16) int len[columns_of(D) + 32];
 };
 
-// Rows of a request: workgroup = (request, `steps` tiles of tokens), all heads.
-template <int D, class T, class C>
+// Rows of a request: workgroup = (request, `steps` tiles of tokens), all heads.  SPLIT waves have the same
+// tokens (then steps is 1), and share out the heads, or a head's columns.
+template <int D, class T, class C, int SPLIT>
 __global__ __launch_bounds__(kBlock) void weigh_rows_kernel(WeighArgs a) {
-    constexpr int NT = kTokens, COLS = columns_of(D);
+    constexpr int NT = kTokens, COLS = columns_of(D), TILE = kTile / SPLIT;
     typedef typename Act<T>::frag frag;
     __shared__ Columns<D> b;
+    __shared__ float shared[SPLIT > 1 ? SPLIT : 1][32 * NT];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, g = lane >> 5;
     const int r = blockIdx.y;
     const int row0 = min(max(a.row_starts[r], 0), a.n_rows), row1 = min(max(a.row_starts[r + 1], row0), a.n_rows);
@@ -83,7 +85,7 @@ __global__ __launch_bounds__(kBlock) void weigh_rows_kernel(WeighArgs a) {
     }
     longest = __builtin_amdgcn_readfirstlane(longest);
     shortest = __builtin_amdgcn_readfirstlane(shortest);
-    const int64_t first = (int64_t)blockIdx.x * kTile * a.steps;
+    const int64_t first = (int64_t)blockIdx.x * TILE * a.steps;
     if (first >= longest) return;
     const int *pages = a.table + (int64_t)r * a.table_stride;
     float *weights = a.weights + a.weight_offsets[r];
@@ -119,7 +121,7 @@ __global__ __launch_bounds__(kBlock) void weigh_rows_kernel(WeighArgs a) {
             }
             __syncthreads();
             for (int s = 0; s < a.steps; ++s) {
-                const int64_t base = first + (int64_t)s * kTile + 32 * NT * wave;
+                const int64_t base = first + (int64_t)s * TILE + 32 * NT * (SPLIT > 1 ? wave / SPLIT : wave);
                 if (base >= longest) break;
                 const int tok = (int)base + NT * n;
                 const int pg = pages[min((int64_t)tok, cap - 1) >> a.lp];
@@ -131,6 +133,11 @@ __global__ __launch_bounds__(kBlock) void weigh_rows_kernel(WeighArgs a) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t) sum[t] = 0.0f;
                 for (int h = 0; h < heads; ++h) {
+                    int c = 0;  // the wave's first columns: every SPLIT-th 32 of all heads'
+                    if constexpr (SPLIT > 1) {
+                        c = 32 * ((wave - h * ((cols + 31) / 32)) & (SPLIT - 1));
+                        if (c >= cols) continue;
+                    }
                     u32x4 raw[NT][D / 32];
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
@@ -146,7 +153,7 @@ __global__ __launch_bounds__(kBlock) void weigh_rows_kernel(WeighArgs a) {
                             k[t][2 * j] = eight<C, T>(raw[t][j][0], raw[t][j][1]);
                             k[t][2 * j + 1] = eight<C, T>(raw[t][j][2], raw[t][j][3]);
                         }
-                    for (int c = 0; c < cols; c += 32) {
+                    for (; c < cols; c += 32 * SPLIT) {
                         const int left = cols - c, at = h * cols + c;
                         f32x16 x[NT];
 #pragma unroll
@@ -182,7 +189,21 @@ __global__ __launch_bounds__(kBlock) void weigh_rows_kernel(WeighArgs a) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     sum[t] += __shfl_xor(sum[t], 32);
-                    if (g == 0 && there && tok + t < longest) weights[tok + t] += sum[t];
+                    if constexpr (SPLIT > 1) {
+                        if (g == 0) shared[wave][NT * n + t] = sum[t];
+                    } else if (g == 0 && there && tok + t < longest) weights[tok + t] += sum[t];
+                }
+                if constexpr (SPLIT > 1) {
+                    // (the next pass' columns wait for all waves, so nobody writes this while it is read)
+                    static_assert(SPLIT == kBlock / 64, "all waves have the same tokens");
+                    __syncthreads();
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        float all = shared[0][NT * n + t];
+#pragma unroll
+                        for (int i = 1; i < SPLIT; ++i) all += shared[i][NT * n + t];
+                        if (tid < 32 && there && tok + t < longest) weights[tok + t] += all;
+                    }
                 }
             }
         }
@@ -858,8 +879,10 @@ Sizes sizes_of(int64_t n_rows, int64_t n_requests, int per, int cols) {
 
 // Requests of up to so many rows x heads read the cache by themselves, without queries in windows (64 of 16384
 // tokens, 16 heads: 8 rows each 96 us, and 180 in windows; 16 rows 169 and 203; one of 131072 tokens, 32 heads:
-// 8 rows 40 and 52, 16 rows 66 and 57).
+// 8 rows 40 and 52, 16 rows 66 and 57), where tokens make workgroups enough (four requests of up to 2635 tokens, 16
+// heads, 7 to 68 rows: 52 us, and 27 with all in windows).
 constexpr int kFew = 256;
+inline int64_t tiles_of(int64_t cap, int n_requests) { return (cap + kTile - 1) / kTile * n_requests; }
 
 // Whether a call may have others.  (Where rows are no more than requests, as single tokens are, none is looked
 // for: the plan would cost as much as a short call.)
@@ -870,9 +893,16 @@ int launch_types(BlockArgs &b, bool block, int n_requests, void *stream) {
     WeighArgs &a = b.a;
     const int64_t cap = (int64_t)a.table_width << a.lp;
     while (a.steps < 4 && cap / (2 * a.steps * kTile) * n_requests >= 1024) a.steps *= 2;
-    const int64_t tokens = (int64_t)kTile * a.steps;
-    const int rc = launch(weigh_rows_kernel<D, T, C>, dim3((unsigned)((cap + tokens - 1) / tokens), (unsigned)n_requests),
-                          dim3(kBlock), stream, a);
+    // Where workgroups are fewer than half of the CUs, the heads over four times as many waves (one row of
+    // 31 tokens, 128 heads: 17 us, and 26 without; 52 rows of up to 162 tokens, 32 heads: 8.9 and 13.9; but 29 of 1874
+    // tokens, 64 heads, 232 workgroups: 17.8 and 14.5).
+    const bool split = a.kv_heads > 1 && tiles_of(cap, n_requests) <= 128;
+    const int64_t tokens = split ? kTile / 4 : (int64_t)kTile * a.steps;
+    const dim3 grid((unsigned)((cap + tokens - 1) / tokens), (unsigned)n_requests);
+    int rc = PAGED_KV_OK;
+    if (a.limit > 0)
+        rc = split ? launch(weigh_rows_kernel<D, T, C, 4>, grid, dim3(kBlock), stream, a)
+                   : launch(weigh_rows_kernel<D, T, C, 1>, grid, dim3(kBlock), stream, a);
     if (rc != PAGED_KV_OK || !block) return rc;
     return launch(weigh_block_kernel<D, T, C>, dim3((unsigned)device_cus() * 2), dim3(kBlock), stream, b);
 }
@@ -917,12 +947,13 @@ extern "C" int serve_weigh(const paged_kv_cache *cache, int32_t act, const void 
     const size_t need = serve_weigh_workspace(n_rows, n_requests, heads, cache->n_heads);
     if (need == 0) return PAGED_KV_EUNSUPPORTED;
     if (block && workspace_bytes < need) return PAGED_KV_EWORKSPACE;
+    const int64_t cap = (int64_t)table_width << lp;
     const double exact = (double)scale * 1.4426950408889634;
     const float scale2 = (float)exact;
     BlockArgs b = {};
     b.a = {(const uint8_t *)cache->k, cache->k_scale, cache->page_stride, cache->scale_stride, cache->n_pages,
            lp, cache->n_heads, q, q_row, q_head, heads, heads / cache->n_heads, lse, table, table_stride,
-           table_width, row_starts, row_lengths, n_rows, 1, block ? kFew : INT64_MAX,
+           table_width, row_starts, row_lengths, n_rows, 1, !block ? INT64_MAX : tiles_of(cap, n_requests) >= 512 ? kFew : 0,
            (u32)(cache->page_stride / cache->head_dim), scale2, scale2 > 0.0f ? (float)(exact / scale2 - 1.0) : 0.0f,
            weights, weight_offsets};
     if (block) {

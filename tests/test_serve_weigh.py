@@ -218,13 +218,17 @@ def test_repeats_to_the_bit_captured_and_on_other_streams():
             assert torch.equal(w, ref), i
 
 
-def test_requests_of_few_and_of_many_rows_in_one_call():
-    """Each kind is a kernel's own: single rows, rows x heads of 256 and of 264, a prompt, none."""
-    s = Setup([900, 300, 513, 1400, 40, 77], [1, 32, 33, 500, 0, 2], page=32, kv=2, heads=8, dim=64, values=False).cuda()
-    assert check(s) == sum(s.lens) - 40
-    # in all no more rows than requests: one request has all of them
-    s = Setup([600] + [20] * 63, [60] + [0] * 63, page=16, kv=1, heads=8, dim=128, values=False).cuda()
-    assert check(s) == 600
+@pytest.mark.parametrize("lens,rows", [
+    ([900, 300, 513, 1400, 40, 77], [1, 32, 33, 500, 0, 2]),   # few tokens: every request in windows
+    ([2040, 900, 300, 513, 1400, 40, 77] + [100] * 57, [3, 1, 32, 33, 500, 0, 2] + [1] * 57),  # rows x heads of 256 and 264
+    ([600] + [20] * 63, [60] + [0] * 63),                      # no more rows than requests: one has all of them
+    ([700, 50, 31], [20, 4, 5]), ([40000], [25]), ([40000, 9], [31, 1]),  # rows x heads of 256 in all
+], ids=str)
+@pytest.mark.parametrize("kv,dim", [(2, 64), (8, 128), (1, 256)], ids=str)
+def test_requests_of_few_and_of_many_rows(lens, rows, kv, dim):
+    """Each kind is a kernel's own, in one call where requests are of both; waves that have the same tokens."""
+    s = Setup(lens, rows, page=32, kv=kv, heads=8, dim=dim, values=False).cuda()
+    assert check(s) == sum(n for n, r in zip(lens, rows) if r)
 
 
 def test_more_parts_than_the_workspace_holds():
