@@ -296,11 +296,13 @@ __global__ __launch_bounds__(kPlan) void plan_kernel(BlockArgs b) {
     __shared__ int64_t waves[kPlan / 64];
     __shared__ int first[kPlan + 1], most_of[kPlan];  // of a round: windows before a request's, its longest row
     __shared__ unsigned long long seen_by[kPlan];     // steps that its windows see, then those of the requests before
+    __shared__ int window_max[kPlan];                 // of a round's first windows
     const WeighArgs &a = b.a;
     const Plan &p = b.p;
     const int tid = threadIdx.x;
     const int64_t cap = (int64_t)a.table_width << a.lp;
     int64_t windows = 0, work = 0, all = 0;
+    Request only = {};  // a request of the only round
     for (int r0 = 0; r0 < b.n; r0 += kPlan) {
         const int r = r0 + tid, here = min(kPlan, b.n - r0);
         int row0 = 0, row1 = 0;
@@ -319,8 +321,9 @@ __global__ __launch_bounds__(kPlan) void plan_kernel(BlockArgs b) {
         windows = min(windows + all, (int64_t)b.max_windows);
         if (tid == 0) first[here] = (int)windows;  // (thread `here`, if there is one, writes the same)
         __syncthreads();
-        // the lengths of a window's rows: 16 lanes to a window
-        for (int w0 = first[0] + tid / 16; w0 < (int)windows; w0 += kPlan / 16) {
+        // the lengths of a window's rows: 8 lanes to a window, 8 lengths of a lane at once
+        constexpr int LANES = 8, AHEAD = 8;
+        for (int w0 = first[0] + tid / LANES; w0 < (int)windows; w0 += kPlan / LANES) {
             int lo = 0, hi = here;
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
@@ -330,17 +333,23 @@ __global__ __launch_bounds__(kPlan) void plan_kernel(BlockArgs b) {
             const int at = start + (b.parts > 1 ? i / b.parts : i * b.rows);
             const int end = min(at + (b.parts > 1 ? 1 : b.rows), stop);
             int most = 0, least = 0x7FFFFFFF;
-#pragma unroll 4
-            for (int row = at + tid % 16; row < end; row += 16) {
-                const int len = (int)min((int64_t)max(a.row_lengths[row], 0), cap);
-                most = max(most, len);
-                least = min(least, len);
+            for (int row0 = at + tid % LANES; row0 < end; row0 += LANES * AHEAD) {
+                int len[AHEAD];
+#pragma unroll
+                for (int j = 0; j < AHEAD; ++j) len[j] = a.row_lengths[min(row0 + LANES * j, end - 1)];
+#pragma unroll
+                for (int j = 0; j < AHEAD; ++j) {
+                    const int x = (int)min((int64_t)max(len[j], 0), cap);
+                    most = max(most, x);
+                    least = min(least, x);
+                }
             }
-            for (int d = 8; d; d >>= 1) {
+            for (int d = LANES / 2; d; d >>= 1) {
                 most = max(most, __shfl_xor(most, d));
                 least = min(least, __shfl_xor(least, d));
             }
-            if (tid % 16 == 0) {
+            if (tid % LANES == 0) {
+                if (w0 - first[0] < kPlan) window_max[w0 - first[0]] = most;
                 p.window_max[w0] = most;
                 p.window_min[w0] = least;
                 atomicMax(&most_of[lo], most);
@@ -352,7 +361,8 @@ __global__ __launch_bounds__(kPlan) void plan_kernel(BlockArgs b) {
         prefix(r < b.n ? (int64_t)steps_of(most_of[tid]) * count * a.kv_heads : 0, waves, &all);
         work += all;
         // (the second round puts in the bases: until then what it needs for them)
-        if (r < b.n) p.requests[r] = {(int64_t)seen_by[tid], most_of[tid], from, count, 0, row0, row1};
+        only = {(int64_t)seen_by[tid], most_of[tid], from, count, 0, row0, row1};
+        if (r < b.n && b.n > kPlan) p.requests[r] = only;
         __syncthreads();
         const unsigned long long before = prefix((int64_t)seen_by[tid], waves, &all);
         __syncthreads();
@@ -363,7 +373,7 @@ __global__ __launch_bounds__(kPlan) void plan_kernel(BlockArgs b) {
         for (int w0 = first[0]; w0 < (int)windows; w0 += kPlan) {
             const int w = w0 + tid;
             int64_t steps = 0;
-            if (w < (int)windows) steps = steps_of(p.window_max[w]);
+            if (w < (int)windows) steps = steps_of(w0 == first[0] ? window_max[tid] : p.window_max[w]);
             const int64_t at = line + prefix(steps, waves, &all);
             line += all;
             if (w < (int)windows) {
@@ -385,7 +395,7 @@ __global__ __launch_bounds__(kPlan) void plan_kernel(BlockArgs b) {
         Request q = {};
         int64_t mine = 0, in_parts = 0, steps = 0;
         if (r < b.n) {
-            q = p.requests[r];
+            q = b.n > kPlan ? p.requests[r] : only;
             const int64_t pieces = ((int64_t)q.part_base * a.kv_heads + size - 1) / size;
             steps = steps_of(q.longest);
             mine = size == 1 ? q.base * a.kv_heads : pieces * ((steps + kRange - 1) / kRange);
@@ -640,8 +650,9 @@ __global__ __launch_bounds__(kBlock, 2) void weigh_block_kernel(BlockArgs b) {
     // In equal shares, neighbouring ones, which read the same keys, on one XCD (workgroups go round them).
     const int eighth = gridDim.x / 8, i8 = blockIdx.x;
     const int share = i8 < 8 * eighth ? (i8 % 8) * eighth + i8 / 8 : i8;
-    int64_t next = total * share / gridDim.x;
-    const int64_t stop = total * (share + 1) / gridDim.x;
+    // (then units are no more than kParts: 32 bits hold all of this)
+    int64_t next = size == 1 ? (u32)total * (u32)share / gridDim.x : 0;
+    const int64_t stop = size == 1 ? (u32)total * (u32)(share + 1) / gridDim.x : 0;
     int ahead = 0;
     if (size > 1 && tid == 0) ahead = atomicAdd(b.p.counter, 1);
     for (;;) {
@@ -662,8 +673,8 @@ __global__ __launch_bounds__(kBlock, 2) void weigh_block_kernel(BlockArgs b) {
         int64_t from, to;
         int s0, s1, piece;
         if (size == 1) {
-            const int64_t of_head = (b.p.requests[r + 1].base - q.base) / a.kv_heads;  // steps that its windows see
-            const int head = (int)((next - q.base) / of_head), line = (int)(next - q.base - head * of_head);
+            const u32 of_head = (u32)(b.p.requests[r + 1].base - q.base) / (u32)a.kv_heads;  // steps that its windows see
+            const int head = (int)((u32)(next - q.base) / of_head), line = (int)((u32)(next - q.base) - head * of_head);
             const int *before = b.p.window_steps + q.window_base;
             const int w = last_base(windows, line, [&](int i) { return (int64_t)before[i]; });
             s0 = line - before[w];
@@ -686,8 +697,12 @@ __global__ __launch_bounds__(kBlock, 2) void weigh_block_kernel(BlockArgs b) {
         const auto page_of = [&](int s) { return pages[min((int64_t)token(min(s, s1 - 1)), cap - 1) >> a.lp]; };
         const auto in_cache = [&](int pg) { return pg >= 0 && pg < a.n_pages; };
         const int page = page_of(s0);
+        int head = (int)(from / windows), w = (int)(from - (int64_t)head * windows) - 1;
         for (int64_t at = from; at < to; ++at) {
-            const int head = (int)(at / windows), w = (int)(at - (int64_t)head * windows);
+            if (++w == windows) {
+                w = 0;
+                ++head;
+            }
             const int most = b.p.window_max[q.window_base + w], least = b.p.window_min[q.window_base + w];
             const int width = b.parts > 1 ? min(window_heads, a.per - w % b.parts * window_heads)
                                           : min(b.rows, q.row1 - q.row0 - w * b.rows) * a.per;
