@@ -3,13 +3,16 @@
 // keep_kernel: a workgroup to a request marks its kept tokens as bits in LDS (a
 // token that is named twice is one bit) and reads them off in order, by a prefix sum
 // over words.  Weights move in place: the i-th kept token is not before place i, so
-// rounds in rising order read nothing that an earlier one has written.
+// rounds in rising order read nothing that an earlier one has written.  Bound by the chain of trips to memory
+// and barriers: 5.8 us for 4 requests of up to 4096 tokens, 10 for 64 of up to 32768.
 //
 // compact_kernel: a workgroup to a request, head and side.  Its waves take the pages
 // that follow each other, up to 8 KB of codes each in registers, all at once; after
 // a barrier they write them.  What a round writes lies before everything that later
 // rounds read, for the same reason, so the next round's loads are on their way
-// meanwhile.  Bound by memory: the codes read, in rows of head_dim bytes, and written.
+// meanwhile.  The codes read, in rows of head_dim bytes, and written bound it (64 requests of 2560 tokens, 2 heads
+// of 128, e4m3: 31 us, 5.3 TB/s), with int8 beside vector work, 10 instructions a code (64 of 4096, 8 heads:
+// 251 us, 4.2 TB/s; a 16-wave workgroup and few of them: trips to memory, 12 us).
 #include "../../include/serve_step.h"
 #include "paged_codes.h"
 
@@ -164,14 +167,19 @@ __device__ inline float largest<Int8>(u32x4 x) {
     return (float)(max(max((int)hi[0], (int)hi[1]), -min((int)lo[0], (int)lo[1])) >> 8);
 }
 
-// Codes of (code * old) / s, 16 at a time; no quotient is past the type's largest.
+// Codes of (code * old) / s, 16 at a time; no quotient is past the type's largest.  `ratio` is ratio_of(old, s).
 template <class C>
-__device__ u32x4 anew(u32x4 x, float old, float s);
+__device__ float ratio_of(float old, float s);
+template <class C>
+__device__ u32x4 anew(u32x4 x, float old, float s, float ratio);
 template <>
-__device__ inline u32x4 anew<E4M3>(u32x4 x, float old, float s) {
+__device__ inline float ratio_of<E4M3>(float old, float s) {
     // s is a power of two, so that the factor is exact, and the product with it rounds as the
     // one with `old` does: once to FP32, once to a code.  (A factor this large is one of codes 0.)
-    const float by = fminf(old * __uint_as_float((254u << 23) - __float_as_uint(s)), 1e30f);
+    return fminf(old * __uint_as_float((254u << 23) - __float_as_uint(s)), 1e30f);
+}
+template <>
+__device__ inline u32x4 anew<E4M3>(u32x4 x, float, float, float by) {
     u32x4 z;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -183,13 +191,15 @@ __device__ inline u32x4 anew<E4M3>(u32x4 x, float old, float s) {
     return z;
 }
 template <>
-__device__ inline u32x4 anew<Int8>(u32x4 x, float old, float s) {
-    // The product with the rounded ratio is within 1.2e-5 of the quotient (2^-24 of 127, and half a
-    // step at 127), so it rounds to the same unless it lies that near a half.  Added to
-    // 1.5 * 2^23 a product has its whole number in the lowest byte.  (Codes as unsigned
-    // bytes, 128 too large, take one instruction to convert; 128 ratios less is exact.)
+__device__ inline float ratio_of<Int8>(float old, float s) {
+    return fminf(__fdiv_rn(old, s), 1e30f);  // (this large: codes are 0)
+}
+template <>
+__device__ inline u32x4 anew<Int8>(u32x4 x, float old, float s, float ratio) {
+    // The product with the rounded ratio is within 7.6e-6 of the quotient (2^-24 of 127), so it rounds to the
+    // same unless it lies that near a half.  Added to 1.5 * 2^23 a product has its whole number in
+    // the lowest byte.
     constexpr float kWhole = 12582912.0f;
-    const float ratio = fminf(__fdiv_rn(old, s), 1e30f), less = -128.0f * ratio;  // (this large: codes are 0)
     u32x4 z;
     float off = 0.0f;
     const auto packed = [](const u32 (&y)[4]) {
@@ -197,17 +207,16 @@ __device__ inline u32x4 anew<Int8>(u32x4 x, float old, float s) {
     };
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const u32 u = x[j] ^ 0x80808080u;
         u32 y[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float q = fmaf((float)((u >> (8 * i)) & 0xFFu), ratio, less), n = q + kWhole;
+            const float c = value_of<Int8>((x[j] >> (8 * i)) & 0xFFu), n = fmaf(c, ratio, kWhole);
             y[i] = __float_as_uint(n);
-            off = fmaxf(off, fabsf(q - (n - kWhole)));
+            off = fmaxf(off, fabsf(fmaf(c, ratio, kWhole - n)));
         }
         z[j] = packed(y);
     }
-    if (!(off < 0.49998f)) {
+    if (!(off < 0.49999f)) {
         // code * old against h * s, h the half next to the product: its rounded product with s
         // taken from both, what is left of either is exact
 #pragma unroll
@@ -366,7 +375,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
         // all of this round is read, and its maxima are there
         meet();
         const int group = (D << a.lp) / 1024;  // entries of `tops` to a page, a power of two
-        float s = 0.0f;
+        float s = 0.0f, ratio = 0.0f;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             if (i == 0 || group < PIECES) {  // (a larger page's are all the same)
@@ -374,6 +383,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
                 float m = 0.0f;
                 for (int j = 0; j < group; ++j) m = fmaxf(m, tops[turn][at + j]);
                 s = scale_of<C>(m);
+                if (SLOTS == 1) ratio = ratio_of<C>(old[0], s);  // lane: of a token, as old
             }
             __builtin_amdgcn_sched_barrier(0);  // one after the other: registers
             // a piece lies in one page
@@ -381,8 +391,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
             const int64_t t = mine + 1024 * i / D;
             if (page < 0 || page >= a.n_pages) continue;
             // (codes under the scale that the page gets are what they are)
-            const float was = scale_at(i);
-            const u32x4 y = was == s ? x[i] : anew<C>(x[i], was, s);
+            const float was = scale_at(i), by = SLOTS == 1 ? __shfl(ratio, (1024 * i + 16 * lane) / D) : ratio_of<C>(was, s);
+            const u32x4 y = was == s ? x[i] : anew<C>(x[i], was, s, by);
             const u32 row = (u32)page * a.page_rows + head_row + (u32)(t & (P - 1));
             if (t + 16 * lane / D < count) __builtin_nontemporal_store(y, (u32x4 *)(codes + (int64_t)row * D + 16 * lane));
             if ((t & (P - 1)) == 0 && lane == 0) scales[page * a.scale_stride] = s;
@@ -393,9 +403,9 @@ __global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
 template <class C, int D>
 int launch_compact(const CompactArgs &a, int n_requests, void *stream) {
     const dim3 grid((unsigned)(a.n_heads * a.sides), (unsigned)n_requests);
-    // 16 waves where workgroups are few, so that one has more on its way (four requests of 604
-    // tokens 12.6 us, and 15.5 with 8 waves); 8 where there are more than the card holds at a time,
-    // so that one computes while another waits (1024 of 4096 tokens 274 us, and 304 with 16)
+    // 16 waves where workgroups are few, so that one has more on its way (with keep: four requests of 604
+    // tokens 17.0 us, and 20.8 with 8 waves); 8 where there are more than the card holds at a time,
+    // so that one computes while another waits (1024 of 4096 tokens 255 us, and 277 with 16)
     const bool small = (int64_t)grid.x * n_requests >= 512 && (D << a.lp) <= 32768;
     return small ? launch(compact_kernel<C, D, 8, 4>, grid, dim3(512), stream, a)
                  : launch(compact_kernel<C, D, 16, 4>, grid, dim3(1024), stream, a);
