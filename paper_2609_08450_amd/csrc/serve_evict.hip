@@ -11,7 +11,7 @@
 // a barrier they write them.  What a round writes lies before everything that later
 // rounds read, for the same reason, so the next round's loads are on their way
 // meanwhile.  The codes read, in rows of head_dim bytes, and written bound it (64 requests of 2560 tokens, 2 heads
-// of 128, e4m3: 31 us, 5.3 TB/s), with int8 beside vector work, 10 instructions a code (64 of 4096, 8 heads:
+// of 128, e4m3: 31 us, 5.3 TB/s), with int8 beside vector work, 13 instructions a code (64 of 4096, 8 heads:
 // 251 us, 4.2 TB/s; a 16-wave workgroup and few of them: trips to memory, 12 us).
 #include "../../include/serve_step.h"
 #include "paged_codes.h"

@@ -7,7 +7,8 @@
 // chain if it has the bit (212 biases of a row of 5099: 5.4 us, and 24 with one list of them).
 // Where a chunk has more biases than entries, a second pass adds them: the words then hold the greatest number
 // of an entry that names the token.  Every workgroup of a row reads the row's whole lists, out of the L2.
-// Bound by memory: a logit read and an FP32 number written.
+// Bound by memory: a logit read and an FP32 number written (256 rows of 131072, lists of 8192 tokens and 100
+// biases: 42.5 us, 4.85 TB/s; 4 rows of 32003: 4.6 us, of trips to memory).
 #include "../../include/serve_step.h"
 #include "paged_common.h"
 
