@@ -155,16 +155,16 @@ __device__ inline float largest<E4M3>(u32x4 x) {
 }
 template <>
 __device__ inline float largest<Int8>(u32x4 x) {
-    // as the high bytes of 16 bits; what lies in the low ones does not reach the next code
+    // as the high bytes of 16 bits: what lies in the low ones decides between equal codes only
     i16x2 hi = {0, 0}, lo = {0, 0};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const i16x2 a = __builtin_bit_cast(i16x2, x[i] & 0xFF00FF00u);
-        const i16x2 b = __builtin_bit_cast(i16x2, (x[i] << 8) & 0xFF00FF00u);
+        const u32 odd = x[i], even = odd << 8;  // (a bit cast of x[i] itself takes x[0])
+        const i16x2 a = __builtin_bit_cast(i16x2, odd), b = __builtin_bit_cast(i16x2, even);
         hi = __builtin_elementwise_max(__builtin_elementwise_max(hi, a), b);
         lo = __builtin_elementwise_min(__builtin_elementwise_min(lo, a), b);
     }
-    return (float)(max(max((int)hi[0], (int)hi[1]), -min((int)lo[0], (int)lo[1])) >> 8);
+    return (float)max(max((int)hi[0], (int)hi[1]) >> 8, -(min((int)lo[0], (int)lo[1]) >> 8));
 }
 
 // Codes of (code * old) / s, 16 at a time; no quotient is past the type's largest.  `ratio` is ratio_of(old, s).
