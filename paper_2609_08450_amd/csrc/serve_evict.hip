@@ -259,8 +259,8 @@ __device__ inline void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier"
 // WAVES of a workgroup hold PIECES of 1024 bytes of codes each, at least a page together.
 template <class C, int D, int WAVES, int PIECES>
 __global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
-    constexpr int TOKENS = PIECES * 1024 / D;  // of a wave's part
-    constexpr int SLOTS = (TOKENS + 63) / 64;
+    constexpr int TOKENS = PIECES * 1024 / D;  // of a wave's part: each has a lane that knows where it lies
+    static_assert(TOKENS <= 64, "a lane to a token");
     __shared__ float tops[2][PIECES * WAVES];
     __shared__ int first_moved;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -295,17 +295,13 @@ __global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
     const int64_t begin = ((int64_t)stay << a.lp) + (int64_t)wave * TOKENS;
     constexpr int64_t ROUND = TOKENS * WAVES;
     const u32 head_row = (u32)(head << a.lp);
-    int kk[SLOTS], pg[SLOTS], pk[SLOTS];  // kept tokens, and pages with the tokens that they are of
-    u32 from[SLOTS];
-    float old[SLOTS], next_old[SLOTS];
+    int kk, pg = -1, pk = -1;  // kept token, and page with the token that it is of
+    u32 from;
+    float old, next_old;
     int to, next_to;  // lane i: the page that piece i goes to
     const auto numbers = [&](int64_t at) {
-#pragma unroll
-        for (int i = 0; i < SLOTS; ++i) {
-            const int64_t t = at + 64 * i + lane;
-            kk[i] = -1;
-            if (lane < TOKENS && t < count) kk[i] = kept[t];
-        }
+        kk = -1;
+        if (lane < TOKENS && at + lane < count) kk = kept[at + lane];
     };
     const auto target = [&](int64_t at) {
         const int64_t t = at + lane * (1024 / D);
@@ -313,29 +309,22 @@ __global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
         if (lane < PIECES && t < count) next_to = table[t >> a.lp];
     };
     const auto look_up = [&] {
-#pragma unroll
-        for (int i = 0; i < SLOTS; ++i) {
-            pk[i] = kk[i];
-            pg[i] = -1;
-            if (kk[i] >= 0 && kk[i] < cap) pg[i] = table[kk[i] >> a.lp];
-        }
+        pk = kk;
+        pg = -1;
+        if (kk >= 0 && kk < cap) pg = table[kk >> a.lp];
     };
     const auto rows = [&] {
-#pragma unroll
-        for (int i = 0; i < SLOTS; ++i) {
-            from[i] = kNone;
-            next_old[i] = 0.0f;
-            if (pg[i] >= 0 && pg[i] < a.n_pages) {
-                from[i] = (u32)pg[i] * a.page_rows + head_row + (u32)(pk[i] & (P - 1));
-                next_old[i] = scales[pg[i] * a.scale_stride];
-            }
+        from = kNone;
+        next_old = 0.0f;
+        if (pg >= 0 && pg < a.n_pages) {
+            from = (u32)pg * a.page_rows + head_row + (u32)(pk & (P - 1));
+            next_old = scales[pg * a.scale_stride];
         }
     };
     const auto fetch = [&](u32x4 (&x)[PIECES]) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const int t = (1024 * i + 16 * lane) / D;  // token of the part
-            const u32 row = __shfl(from[SLOTS == 1 ? 0 : t >> 6], t & 63);
+            const u32 row = __shfl(from, (1024 * i + 16 * lane) / D);  // (token of the part)
             x[i] = u32x4{0, 0, 0, 0};
             if (row != kNone) x[i] = *(const u32x4 *)(codes + (int64_t)row * D + (16 * lane) % D);
         }
@@ -353,8 +342,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
     for (int64_t mine = begin; mine - (int64_t)wave * TOKENS < count; mine += ROUND, turn ^= 1) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) x[i] = next[i];
-#pragma unroll
-        for (int i = 0; i < SLOTS; ++i) old[i] = next_old[i];
+        old = next_old;
         to = next_to;
         rows();
         look_up();
@@ -363,10 +351,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
         fetch(next);
 
         // the largest magnitude of every 1024 bytes
-        const auto scale_at = [&](int i) {
-            const int t = (1024 * i + 16 * lane) / D;
-            return __shfl(old[SLOTS == 1 ? 0 : t >> 6], t & 63);
-        };
+        const auto scale_at = [&](int i) { return __shfl(old, (1024 * i + 16 * lane) / D); };
         float top[PIECES];
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) top[i] = __fmul_rn(largest<C>(x[i]), scale_at(i));
@@ -383,7 +368,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
                 float m = 0.0f;
                 for (int j = 0; j < group; ++j) m = fmaxf(m, tops[turn][at + j]);
                 s = scale_of<C>(m);
-                if (SLOTS == 1) ratio = ratio_of<C>(old[0], s);  // lane: of a token, as old
+                ratio = ratio_of<C>(old, s);  // lane: of a token, as old
             }
             __builtin_amdgcn_sched_barrier(0);  // one after the other: registers
             // a piece lies in one page
@@ -391,7 +376,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void compact_kernel(CompactArgs a) {
             const int64_t t = mine + 1024 * i / D;
             if (page < 0 || page >= a.n_pages) continue;
             // (codes under the scale that the page gets are what they are)
-            const float was = scale_at(i), by = SLOTS == 1 ? __shfl(ratio, (1024 * i + 16 * lane) / D) : ratio_of<C>(was, s);
+            const float was = scale_at(i), by = __shfl(ratio, (1024 * i + 16 * lane) / D);
             const u32x4 y = was == s ? x[i] : anew<C>(x[i], was, s, by);
             const u32 row = (u32)page * a.page_rows + head_row + (u32)(t & (P - 1));
             if (t + 16 * lane / D < count) __builtin_nontemporal_store(y, (u32x4 *)(codes + (int64_t)row * D + 16 * lane));

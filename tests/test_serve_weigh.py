@@ -231,6 +231,18 @@ def test_requests_of_few_and_of_many_rows(lens, rows, kv, dim):
     assert check(s) == sum(n for n, r in zip(lens, rows) if r)
 
 
+def test_more_requests_than_a_round_of_the_plan():
+    """Of 560 requests, a few with more rows than the kernel of few rows takes, at the round's edges among them."""
+    rows = [17 if r in (0, 99, 511, 512, 559) else 0 if r % 5 == 2 else 1 for r in range(560)]
+    s = Setup([(7 * r) % 90 + 20 for r in range(560)], rows, page=16, kv=1, heads=16, dim=64, values=False).cuda()
+    assert sum(rows) <= 560  # read by rows
+    check(s)
+    rows = [r + 40 * (r == 17) for r in rows]
+    s = Setup([(7 * r) % 90 + 60 for r in range(560)], rows, page=16, kv=1, heads=16, dim=64, values=False).cuda()
+    assert sum(rows) > 560
+    check(s)
+
+
 def test_more_parts_than_the_workspace_holds():
     """Windows add up in one part then; beside them a request of one window, one without rows and one whose windows
     are a single piece."""
