@@ -10,7 +10,7 @@
 // exponentials and all sums of them are FP32.
 //
 // weigh_rows_kernel, few rows: bound by memory, the codes read once (64 single rows of 16384 to 131072
-// tokens, 2 heads of 128: 251 us, 4.74 TB/s; the same loads without the products 239 us, or 232 in one
+// tokens, 2 heads of 128: 252 us, 4.71 TB/s; the same loads without the products 239 us, or 232 in one
 // line).  Codes fetched ahead (265 us), pages and old weights ahead (267 to 281), one token to a lane (256)
 // and equal shares for resident workgroups (305) were slower: waves of other workgroups cover the trips.
 //
@@ -86,18 +86,13 @@ __global__ __launch_bounds__(kBlock) void weigh_rows_kernel(WeighArgs a) {
     const int row0 = min(max(a.row_starts[r], 0), a.n_rows), row1 = min(max(a.row_starts[r + 1], row0), a.n_rows);
     if ((int64_t)(row1 - row0) * a.heads > a.limit) return;
     const int64_t cap = (int64_t)a.table_width << a.lp;
-    int longest = 0, shortest = 0x7FFFFFFF;
+    int longest = 0;
     for (int i = row0 + lane; i < row1; i += 64) {
         const int len = (int)min((int64_t)max(a.row_lengths[i], 0), cap);
         longest = max(longest, len);
-        shortest = min(shortest, len);
     }
-    for (int d = 32; d; d >>= 1) {
-        longest = max(longest, __shfl_xor(longest, d));
-        shortest = min(shortest, __shfl_xor(shortest, d));
-    }
+    for (int d = 32; d; d >>= 1) longest = max(longest, __shfl_xor(longest, d));
     longest = __builtin_amdgcn_readfirstlane(longest);
-    shortest = __builtin_amdgcn_readfirstlane(shortest);
     const int64_t first = (int64_t)blockIdx.x * TILE * a.steps;
     if (first >= longest) return;
     const int *pages = a.table + (int64_t)r * a.table_stride;
@@ -126,7 +121,8 @@ __global__ __launch_bounds__(kBlock) void weigh_rows_kernel(WeighArgs a) {
                     const int64_t col = col0 + i - h * cols;
                     const int row = row0 + (int)(col / a.per);
                     x = softmax_of(a.lse[(int64_t)row * a.heads + (head0 + h) * a.per + (int)(col % a.per)], a.stretch);
-                    len = (int)min((int64_t)max(a.row_lengths[row], 0), cap);
+                    // (a column without a softmax sees nothing: a key that is NaN would make its product NaN, 0 or not)
+                    if (x.lse2 != __builtin_inff()) len = (int)min((int64_t)max(a.row_lengths[row], 0), cap);
                 }
                 b.lse2[i] = x.lse2;
                 b.fine[i] = x.fine;
@@ -141,7 +137,6 @@ __global__ __launch_bounds__(kBlock) void weigh_rows_kernel(WeighArgs a) {
                 const bool there = pg >= 0 && pg < a.n_pages;
                 const uint8_t *codes = a.k + (there ? pg : 0) * a.page_stride + (int64_t)(tok & ((1 << a.lp) - 1)) * D + 16 * g;
                 const float *scales = a.ks + (there ? pg : 0) * a.scale_stride;
-                const bool masked = base + 32 * NT > shortest && shortest != longest;
                 float sum[NT];
 #pragma unroll
                 for (int t = 0; t < NT; ++t) sum[t] = 0.0f;
@@ -189,7 +184,7 @@ __global__ __launch_bounds__(kBlock) void weigh_rows_kernel(WeighArgs a) {
                                 const int col = 2 * i0 + 4 * g + i;
                                 if (col >= left) break;
                                 const float l = b.lse2[at + col], f = b.fine[at + col];
-                                const int len = masked ? b.len[at + col] : 0x7FFFFFFF;
+                                const int len = b.len[at + col];
 #pragma unroll
                                 for (int t = 0; t < NT; ++t) {
                                     const float p = exp2_(fmaf(x[t][i0 + i], scale, -l)) * f;
@@ -653,7 +648,7 @@ __global__ __launch_bounds__(kBlock, 2) void weigh_block_kernel(BlockArgs b) {
     constexpr int NT = kTokens, PER = D / 8;  // 16-byte pieces of a column
     typedef typename Act<T>::frag frag;
     __shared__ Window<D> o;
-    __shared__ int taken;
+    __shared__ int taken, empty[kBlock / 64];
     const WeighArgs &a = b.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
     const int64_t cap = (int64_t)a.table_width << a.lp;
@@ -755,7 +750,12 @@ __global__ __launch_bounds__(kBlock, 2) void weigh_block_kernel(BlockArgs b) {
                     mine = softmax_of(a.lse[(int64_t)(row0 + row) * a.heads + h], a.stretch);
                     len = (int)min((int64_t)max(a.row_lengths[row0 + row], 0), cap);
                 }
+                // A column without a softmax sees nothing: a key that is NaN would make its product NaN, 0 or not.
+                // (The columns past the window's are not masked for it: such a key makes the others' sum NaN, too.)
+                const bool none = tid < width && mine.lse2 == __builtin_inff(), any = __any(none);
+                if (none) len = 0;
                 __syncthreads();  // the window before is done with
+                if (lane == 0) empty[wave] = any;
                 if (tid < window_of(D)) {
                     o.lse2[tid] = mine.lse2;
                     o.fine[tid] = mine.fine;
@@ -786,11 +786,13 @@ __global__ __launch_bounds__(kBlock, 2) void weigh_block_kernel(BlockArgs b) {
                     for (int j = 0; j < D / 32; ++j) raw[t][j] = *(const u32x4 *)(p + t * D + 32 * j);
                 raw_scale = a.ks[page * a.scale_stride + head];
             };
-            int next_page = page;
+            int next_page = page, seen_by_all = least;
             if (sees) {
                 fetch(s0, page);
                 next_page = page_of(s0 + 1);
                 __syncthreads();
+                for (int i = 0; i < kBlock / 64; ++i) seen_by_all = empty[i] ? 0 : seen_by_all;
+                seen_by_all = __builtin_amdgcn_readfirstlane(seen_by_all);
             }
 #pragma unroll 1
             for (int s = s0; s < end; ++s) {
@@ -811,7 +813,7 @@ __global__ __launch_bounds__(kBlock, 2) void weigh_block_kernel(BlockArgs b) {
                     fetch(min(s + 1, end - 1), next_page);
                     next_page = page_of(s + 2);
                 }
-                if (base + 32 * NT <= least) pass<D, T>(o, cols, k, scale, sum);
+                if (base + 32 * NT <= seen_by_all) pass<D, T>(o, cols, k, scale, sum);
                 else if (base < most) pass_masked<D, T>(o, cols, k, scale, sum, tok);
                 if (D == 256) {
                     fetch(min(s + 1, end - 1), next_page);

@@ -120,6 +120,26 @@ def test_rows_without_a_softmax():
             assert bool(((w[r, :len(sums[r])].double() - sums[r]).abs() <= 1e-3 * sums[r] + 1e-30).all())
 
 
+@pytest.mark.parametrize("lens,rows,heads,dim", [
+    ([100, 90], [1, 1], 8, 64), ([100] * 300, [1] * 300, 4, 64), ([100, 90], [4, 1], 8, 128), ([100, 600], [70, 40], 8, 128),
+    ([100, 600], [30, 40], 16, 256), ([600], [40], 2, 64)], ids=str)
+def test_rows_without_a_softmax_see_keys_that_are_nan(lens, rows, heads, dim):
+    """An lse of -inf adds nothing, whatever the keys hold: rows that see codes behind a request's tokens, NaN here, by
+    themselves, among others of their window, and as all of a window."""
+    s = Setup(lens, rows, page=16, kv=2, heads=heads, dim=dim, values=False).cuda()
+    cap, starts = s.table.shape[1] * 16, s.row_starts.tolist()
+    lse = lse_of(s)
+    for r, n in enumerate(lens):
+        # the pages' last tokens are what nobody has stored
+        s.row_lengths[starts[r]] = -(-n // 16) * 16 if n % 16 else min(n, cap)
+        lse[starts[r]] = -math.inf
+    check(s, lse)
+    for r, n in enumerate(lens):
+        s.row_lengths[starts[r]:starts[r + 1]] = -(-n // 16) * 16
+    lse[:] = -math.inf
+    check(s, lse)
+
+
 def test_pages_outside_the_cache():
     for rows in ([1, 1], [50, 30]):
         s = Setup([100, 333], rows, page=16, kv=2, heads=4, dim=64, values=False)
