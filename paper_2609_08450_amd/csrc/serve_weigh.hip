@@ -60,7 +60,8 @@ __device__ inline Softmax softmax_of(float lse, float stretch) {
     constexpr float lo = 1.9259629911266175e-8f;  // log2(e) - kLog2e
     const float hi = lse * kLog2e;
     const float rest = fmaf(lse, kLog2e, -hi) + lse * lo;
-    return {hi, exp2_(fmaf(hi, stretch, -rest))};
+    // (a factor of 0 or inf, of an lse past 1e9, would make NaN of the inf or the 0 that it belongs to)
+    return {hi, exp2_(fminf(fmaxf(fmaf(hi, stretch, -rest), -126.0f), 126.0f))};
 }
 
 // Query columns in LDS.

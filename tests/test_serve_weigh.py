@@ -140,6 +140,27 @@ def test_rows_without_a_softmax_see_keys_that_are_nan(lens, rows, heads, dim):
     check(s, lse)
 
 
+@pytest.mark.parametrize("rows", [[1, 1], [40, 30]], ids=str)
+def test_softmaxes_of_any_size(rows):
+    """Finite ones up to the largest FP32 number: exp of what is left is 0, or past every number."""
+    from paper_2609_08450_amd import evict
+
+    s = Setup([100, 333], rows, page=16, kv=2, heads=8, dim=64, values=False).cuda()
+    lse = lse_of(s)
+    for i, z in enumerate((1e8, 1.1e9, 1e10, 3.3e10, 7.7e15, 1e20, 1.7e30, 2.4e38, 2.36e38, 3.4e38)):
+        far = torch.full_like(lse, z) * (1 + 2.0 ** -20 * torch.rand(lse.shape, generator=torch.Generator().manual_seed(i)).cuda())
+        far = far.clamp(max=torch.finfo(torch.float32).max)
+        check(s, far, where=str(z))
+        few = lse.clone()
+        few[:, 3], few[-1] = far[:, 3], far[-1]
+        check(s, few, where=f"{z} among others")
+        w = torch.zeros((2, 400), device="cuda")
+        evict.weigh(s.cache(), s.q, -far, s.table, s.row_starts, s.row_lengths, s.scale, w, torch.tensor([0, 400]).cuda())
+        for r in range(2):
+            seen = int(s.row_lengths[s.row_starts[r]:s.row_starts[r + 1]].max())
+            assert bool((w[r, :seen] == math.inf).all()) and not bool(w[r, seen:].any()), z
+
+
 def test_pages_outside_the_cache():
     for rows in ([1, 1], [50, 30]):
         s = Setup([100, 333], rows, page=16, kv=2, heads=4, dim=64, values=False)
