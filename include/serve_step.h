@@ -53,8 +53,10 @@ typedef struct serve_heads {
 /* (a, b) -> m (a cos t - b sin t, a sin t + b cos t) for each pair (a, b) of each
  * row's heads, t its angle, m the magnitude; `transposed` takes -t: the map's
  * transpose, which takes a gradient of the output to that of the input.  Other
- * elements are copied.  Angles are exact to 2^-32 of a turn (but for the rounding of
- * `turns`) at any position; the products are FP32, rounded once to the type.
+ * elements are copied.  Angles are off by at most 2^-28 + 2^-32 of a turn (beside what
+ * the rounding of `turns` comes to) at any position: position * turns is cut to 2^-32,
+ * and its distance from the nearest quarter turn is rounded to FP32.  Cosines,
+ * sines and products are FP32, rounded once to the type.
  *   act        PAGED_KV_BF16, PAGED_KV_F16 or SERVE_F32;
  *   positions  int32, or int64 where `wide` is not 0, [n_rows], of any sign;
  *   q, k       heads of one row and dim; k may be NULL;

@@ -60,7 +60,7 @@ __device__ typename Piece<T, V>::type packed(const float *y) {
 }
 
 // Cosine and sine of t / 2^32 turns: the quarter turn apart, which is exact, so that
-// what is left converts to a float within 2^-25 of an eighth of a turn.
+// what is left, at most an eighth of a turn, converts to a float within 2^-25 of that: 2^-28 of a turn.
 __device__ inline void cos_sin(int t, float &c, float &s) {
     const int quarter = (int)((u32)t + (1u << 29)) >> 30;  // -2 .. 1
     const int rest = (int)((u32)t - ((u32)quarter << 30));

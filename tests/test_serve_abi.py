@@ -87,6 +87,16 @@ def test_rotate_refusals(serve):
     assert L.serve_rotate(0, None, P, 0, 5, 64, None, None, 0, None) == EINVAL
 
 
+def test_the_angle_s_bound_counts_its_rounding_to_fp32():
+    """A rotation's angle is a whole number of 2^-32 turns, rounded down, and its distance from a quarter turn, at most 2^29 of
+    them, becomes an FP32 number: the header's bound is of both."""
+    rest = torch.arange(2 ** 29 - 2 ** 16, 2 ** 29 + 1, dtype=torch.int64)
+    off = 1 + int((rest.float().long() - rest).abs().max())
+    about = re.sub(r"[ \n*]+", " ", TEXT[TEXT.index("(a, b) -> m"):TEXT.index("int serve_rotate(")])
+    bound = re.search(r"[Aa]ngles are (?:exact to|off by at most) 2\^-(\d+)(?: \+ 2\^-(\d+))? of a turn", about)
+    assert off / 2 ** 32 <= sum(2.0 ** -int(x) for x in bound.groups() if x)
+
+
 def cache_of(**change):
     from paper_2609_08450_amd import paged
 
