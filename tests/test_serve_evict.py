@@ -110,6 +110,17 @@ def test_compact(lens, keep, page, kv, dim, code):
     moved(s, some(lens, keep))
 
 
+@pytest.mark.parametrize("code", [E4M3, torch.int8], ids=str)
+@pytest.mark.parametrize("page,dim", [(16, 64), (256, 64), (32, 128), (256, 128), (128, 256), (256, 256)], ids=str)
+def test_compact_of_many_requests(page, dim, code):
+    """64 requests of 4 heads, K and V: 512 workgroups, which have 8 waves each where a page's codes of a head are at most
+    32768 bytes (a round is then one page at the largest, several at smaller ones).  Most are short, some take several rounds."""
+    lens = [40 + 3 * i for i in range(60)] + [1500, 1300, 1100, 2 * page + 1]
+    keep = [1 + (11 * n) % 90 for n in lens[:60]] + [1290, 640, 513, page + 1]
+    s = Setup(lens, [1] * 64, page=page, kv=4, heads=4, dim=dim, code=code, seed=page + dim).cuda()
+    moved(s, some(lens, keep))
+
+
 def test_compact_of_power_of_two_scales():
     """As the store leaves e4m3 pages."""
     s = Setup([800, 90], [1, 1], page=32, kv=2, heads=2, dim=64)
