@@ -62,6 +62,37 @@ def test_sizes(rows, heads, kv):
 
 
 @gpu
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("act,rows,heads,kv,dim,rot,start", [
+    (torch.bfloat16, 4099, 16, 2, 128, 128, 0), (torch.float16, 40001, 1, 1, 128, 128, 0),
+    (torch.float32, 4097, 7, 2, 160, 64, 32), (torch.bfloat16, 9001, 4, 1, 256, 64, 192)], ids=str)
+def test_large_calls(act, rows, heads, kv, dim, rot, start, layout):
+    """Above 16 MB results are written past the caches.  To the bit what the same rows get in smaller calls, in
+    place and apart, and some of them against the definition."""
+    from paper_2609_08450_amd import rotary
+
+    assert rows * (heads + kv) * dim * torch.finfo(act).bits // 8 > 16 << 20
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn((rows, heads + kv, dim), generator=g, device="cuda").to(act)
+    positions = torch.randint(0, 1 << 20, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    rope = rotary.Rotary(rot, layout=layout, start=start)
+    for transposed in (False, True):
+        small = [rotary.rotate(rope, positions[i:i + 800], x[i:i + 800, :heads], x[i:i + 800, heads:], transposed=transposed)
+                 for i in range(0, rows, 800)]
+        ref = [torch.cat(part) for part in zip(*small)]
+        apart = rotary.rotate(rope, positions, x[:, :heads], x[:, heads:], transposed=transposed)
+        y = x.clone()
+        q, k = y[:, :heads], y[:, heads:]
+        rotary.rotate(rope, positions, q, k, q_out=q, k_out=k, transposed=transposed)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(apart, ref)) and all(torch.equal(a, b) for a, b in zip((q, k), ref))
+        some = [0, 1, 799, rows // 2, rows - 2, rows - 1]
+        want = rotated(unsigned(rope), 1.0, positions[some].tolist(), x[some, :heads].cpu(), start, layout == "interleaved",
+                       transposed)
+        assert_rotated(apart[0][some], want, 1.0)
+
+
+@gpu
 def test_no_rows():
     from paper_2609_08450_amd import rotary
 
