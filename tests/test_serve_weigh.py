@@ -272,6 +272,35 @@ def test_requests_of_few_and_of_many_rows(lens, rows, kv, dim):
     assert check(s) == sum(n for n, r in zip(lens, rows) if r)
 
 
+ENDS = [1, 0, 2, 63, 64, 65, 127, 255, 256, 257, 300, 511, 512, 513, 700, 767, 768, 769, 900, 1023, 1024, 1025, 1279, 1280,
+        1281, 1500, 1793, 2047, 2048, 2049, 2100, 3073]
+
+
+@pytest.mark.parametrize("width", [8192, 16384])
+@pytest.mark.parametrize("kv,heads,dim,code", [(5, 160, 64, E4M3), (1, 130, 64, torch.int8), (4, 80, 256, torch.int8),
+                                               (2, 8, 128, E4M3)], ids=str)
+def test_tables_far_wider_than_the_requests(kv, heads, dim, code, width):
+    """64 requests under a table of 8192 and of 16384 tokens: workgroups of two and of four tiles, lengths that end at
+    every one's edges, and several passes over the queries' columns.  Then with two rows to some requests, which
+    go to either kernel by their heads."""
+    for rows in ([1] * 64, [2, 1, 3, 2, 1, 1, 2, 0] + [1] * 20 + [3] + [1] * 35):
+        s = Setup((ENDS * 2)[:len(rows)], rows, page=16, kv=kv, heads=heads, dim=dim, code=code, values=False)
+        table = torch.full((len(rows), width // 16), -1, dtype=torch.int32)
+        table[:, :s.table.shape[1]] = s.table
+        s.table = table
+        s = s.cuda()
+        assert check(s, where=str(rows[:8])) == sum(n for n, r in zip(s.lens, rows) if r)
+
+
+@pytest.mark.parametrize("kv,heads,dim,lens,rows", [
+    (1, 300, 64, [300, 520], [3, 2]), (1, 257, 64, [33], [4]), (2, 1400, 128, [300], [2]), (1, 130, 256, [300, 40], [5, 1]),
+    (2, 400, 256, [513, 257], [3, 4]), (1, 129, 256, [90], [2])], ids=str)
+def test_more_heads_of_a_cache_head_than_a_window(kv, heads, dim, lens, rows):
+    """Windows of a part of one row's heads, the last part smaller than the others."""
+    s = Setup(lens, rows, page=32, kv=kv, heads=heads, dim=dim, values=False).cuda()
+    assert check(s) == sum(lens)
+
+
 def test_more_requests_than_a_round_of_the_plan():
     """Of 560 requests, a few with more rows than the kernel of few rows takes, at the round's edges among them."""
     rows = [17 if r in (0, 99, 511, 512, 559) else 0 if r % 5 == 2 else 1 for r in range(560)]
@@ -319,6 +348,42 @@ def test_more_parts_than_the_workspace_holds():
         off = (w[r, :L].double() - 2 * total[r]).abs() - 2 * bound[r] - (s.n_rows * 128 + 1) * 2.0 ** -23 * total[r]
         assert bool((off <= 0).all()) and not bool(w[r, L:].any()), r
     assert not bool(w[2].any())
+
+
+def test_more_parts_than_the_workspace_holds_of_parts_of_rows():
+    """Windows that add up in one part, each of a part of one row's heads.  (A few heads are compared: the others' lse is
+    so large that they add nothing, and what they could add is below FP32's least.)"""
+    from paper_2609_08450_amd import evict
+
+    s = Setup([20000, 300], [320, 3], page=256, kv=1, heads=300, dim=64, values=False).cuda()
+    assert sum(2 * n * -(-L // 256) for L, n in zip(s.lens, (320, 3))) > 49152
+    picked = (0, 149, 150, 151, 299)
+    lse = torch.full((s.n_rows, 300), 1e4, device="cuda")
+    w = torch.zeros((2, 20000), device="cuda")
+    sums = []
+    for r in range(2):
+        a, b, L = int(s.row_starts[r]), int(s.row_starts[r + 1]), s.lens[r]
+        k, there = s.tokens("k", r, L)
+        assert bool(there.all())
+        hidden = torch.arange(L, device="cuda") >= s.row_lengths[a:b, None]
+        total, bound = torch.zeros(L, dtype=torch.float64, device="cuda"), torch.zeros(L, dtype=torch.float64, device="cuda")
+        for h in picked:
+            q = s.q[a:b, h].double()
+            x = s.scale * torch.matmul(q, k[0].t())
+            z = torch.logsumexp(x.masked_fill(hidden, -math.inf), 1)
+            lse[a:b, h] = z.float()
+            z = lse[a:b, h, None].double()
+            p = torch.exp(x - z).masked_fill(hidden, 0.0)
+            size = s.scale * torch.matmul(q.abs(), k[0].abs().t())
+            total += p.sum(0)
+            bound += (p * (64 * 2.0 ** -24 * size + 2.0 ** -22 * (x.abs() + z.abs()) + 2.0 ** -21)).sum(0)
+        # FP32 sums of each row's 300 heads, a rounding to a term, and of the old weight
+        sums.append((total, bound + (len(q) * 300 + 1) * 2.0 ** -24 * total + 2.0 ** -24 * total))
+    evict.weigh(s.cache(), s.q, lse, s.table, s.row_starts, s.row_lengths, s.scale, w, torch.tensor([0, 20000]).cuda())
+    torch.cuda.synchronize()
+    for r, (total, bound) in enumerate(sums):
+        L = s.lens[r]
+        assert bool(((w[r, :L].double() - total).abs() <= bound).all()) and not bool(w[r, L:].any()), r
 
 
 def test_far_offsets():
