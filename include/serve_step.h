@@ -82,6 +82,8 @@ size_t serve_weigh_workspace(int32_t n_rows, int32_t n_requests, int32_t heads, 
  * FP32 products, exponentials and sums.
  *   q, act, table, row_starts, row_lengths, scale  as in paged_kv_attend; the cache
  *                   need not have values;
+ *   table_width     what the launch is laid out for, as the host knows no lengths: a table far
+ *                   wider than the longest request costs time;
  *   lse             FP32 [n_rows][heads];
  *   weight_offsets  int64 [n_requests], in elements; no two requests' weights overlap. */
 int serve_weigh(const paged_kv_cache *cache, int32_t act, const void *q, int64_t q_row,

@@ -175,8 +175,9 @@ __global__ __launch_bounds__(kBlock) void adjust_kernel(AdjustArgs a) {
             out_t z;
 #pragma unroll
             for (int j = 0; j < V; ++j) z[j] = y[j];
-            // past the caches where a call's rows are more than they hold (256 rows of 131072: 43 us, and
-            // 61 with stores that stay in them)
+            // past the caches where a call's rows are more than they hold (256 rows of 131072 with all lists: 43 us,
+            // and 61 with stores that stay in them; without lists and with a Top-K behind it 64.3 and 65.9, but 27.4
+            // and 25.4 for 64 rows, which the last-level cache holds)
             if constexpr (E == 16) __builtin_nontemporal_store(z, (out_t *)(out + at));
             else *(out_t *)(out + at) = z;
         } else

@@ -241,7 +241,8 @@ extern "C" int serve_rotate(int32_t act, const serve_rotary *rotary, const void 
                n_rows / (2 * a.rows) >= 1024)
             a.rows *= 2;
     // what the L2s (32 MB) do not hold anyway goes past them (8192 rows of 40 heads of 128: 33.5 us,
-    // and 39.9 with stores that stay in them)
+    // and 39.9 with stores that stay in them; with the store of its keys and one reader of its queries behind
+    // it 91 and 99, but 35.2 and 31.7 for 2048 rows, 21 MB, which the last-level cache holds)
     const bool past = (int64_t)n_rows * a.heads * dim * size > 16 << 20;
     const dim3 grid((unsigned)(((int64_t)n_rows + a.rows - 1) / a.rows), (unsigned)((a.heads + a.per - 1) / a.per));
     if (grid.y > 65535) return PAGED_KV_EUNSUPPORTED;

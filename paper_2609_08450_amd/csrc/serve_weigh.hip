@@ -14,10 +14,11 @@
 // line).  Codes fetched ahead (265 us), pages and old weights ahead (267 to 281), one token to a lane (256)
 // and equal shares for resident workgroups (305) were slower: waves of other workgroups cover the trips.
 //
-// weigh_block_kernel, many rows: bound by matrix and vector work beside each other, 2 instructions a result
-// and an exponential at a quarter of their rate (4096 rows of three prompts, 32 heads of 128: 223 us with
-// the plan's 8 and the join's 9, 905 TFLOP/s; matrix cores busy in 43 % of the cycles, vector instructions
-// issuing in 57 %).  Tiles of keys through LDS and an order left to the compiler took 265 us and more.
+// weigh_block_kernel, many rows: bound by matrix and vector work, 2 instructions a result and an exponential
+// at a quarter of their rate (4096 rows of three prompts, 32 heads of 128: 223 us with the plan's 8 and the
+// join's 9, 905 TFLOP/s; 16 heads of 256: 225 us).  Matrix cores are busy in 43 % of the cycles and vector instructions
+// issue in 57 %, which is all of them: the two follow one another more than they overlap.  Tiles of keys
+// through LDS and an order left to the compiler took 265 us and more.
 #include "../../include/serve_step.h"
 #include "paged_common.h"
 
@@ -911,7 +912,9 @@ Sizes sizes_of(int64_t n_rows, int64_t n_requests, int per, int cols) {
 // Requests of up to so many rows x heads read the cache by themselves, without queries in windows (64 of 16384
 // tokens, 16 heads: 8 rows each 96 us, and 180 in windows; 16 rows 169 and 203; one of 131072 tokens, 32 heads:
 // 8 rows 40 and 52, 16 rows 66 and 57), where tokens make workgroups enough (four requests of up to 2635 tokens, 16
-// heads, 7 to 68 rows: 52 us, and 27 with all in windows).
+// heads, 7 to 68 rows: 52 us, and 27 with all in windows).  This and the rules of launch_types() go by the tokens that
+// the table has room for, since the host knows no lengths; they were measured with tables as wide as the longest
+// request.  Under one of 131072 tokens 4 rows of up to 3392 tokens take 48 us for 7.5, 64 rows of 2000 260 us for 26.
 constexpr int kFew = 256;
 inline int64_t tiles_of(int64_t cap, int n_requests) { return (cap + kTile - 1) / kTile * n_requests; }
 

@@ -47,7 +47,8 @@ def weigh(cache, q, lse, table, row_starts, row_lengths, scale: float, weights, 
           stream=None) -> None:
     """Forwards to serve_weigh(): adds to each request's weights (any contiguous float32 tensor, request r's
     from weight_offsets[r] on) what its tokens got of the attention of q [rows, heads, dim], whose ``lse``
-    float32 [rows, heads] ``paged.attend`` gave.  ``workspace``: uint8 of ``workspace_size`` bytes, for a
+    float32 [rows, heads] ``paged.attend`` gave.  The launch is laid out for the table's width: where a program knows that
+    requests are far shorter, ``table[:, :pages]`` is faster.  ``workspace``: uint8 of ``workspace_size`` bytes, for a
     program that keeps one; where that is 256 (single tokens, few rows) a call uses none."""
     dev = cache._on_current()
     qp, q_row, q_head = _paged._rows3(q, None, cache.head_dim, "q", dev)
