@@ -19,6 +19,8 @@
 // join's 9, 905 TFLOP/s; 16 heads of 256: 225 us).  Matrix cores are busy in 43 % of the cycles and vector instructions
 // issue in 57 %, which is all of them: the two follow one another more than they overlap.  Tiles of keys
 // through LDS and an order left to the compiler took 265 us and more.
+#include <cfloat>
+
 #include "../../include/serve_step.h"
 #include "paged_common.h"
 
@@ -984,11 +986,14 @@ extern "C" int serve_weigh(const paged_kv_cache *cache, int32_t act, const void 
     const int64_t cap = (int64_t)table_width << lp;
     const double exact = (double)scale * 1.4426950408889634;
     const float scale2 = (float)exact;
+    // (a scale below the normal numbers has few bits: what its rounding leaves is then no small part of lse, and scores
+    // are far too small for it to matter)
+    const float stretch = scale2 >= FLT_MIN ? (float)(exact / scale2 - 1.0) : 0.0f;
     BlockArgs b = {};
     b.a = {(const uint8_t *)cache->k, cache->k_scale, cache->page_stride, cache->scale_stride, cache->n_pages,
            lp, cache->n_heads, q, q_row, q_head, heads, heads / cache->n_heads, lse, table, table_stride,
            table_width, row_starts, row_lengths, n_rows, 1, !block ? INT64_MAX : tiles_of(cap, n_requests) >= 512 ? kFew : 0,
-           (u32)(cache->page_stride / cache->head_dim), scale2, scale2 > 0.0f ? (float)(exact / scale2 - 1.0) : 0.0f,
+           (u32)(cache->page_stride / cache->head_dim), scale2, stretch,
            weights, weight_offsets};
     if (block) {
         const Sizes s = sizes_of(n_rows, n_requests, b.a.per, window_of(cache->head_dim));

@@ -211,6 +211,14 @@ def test_scale_zero_and_no_heads_in_common():
     check(s, lse=torch.full((2, 3), 1.5, device="cuda"), scale=0.0)
 
 
+@pytest.mark.parametrize("rows", [[1, 1], [40, 30]], ids=str)
+def test_the_least_scales(rows):
+    """Below FP32's least normal number a scale has few bits: what its rounding leaves is then no factor of the weights."""
+    s = Setup([100, 333], rows, page=16, kv=2, heads=8, dim=64, values=False).cuda()
+    for s.scale in (1.4e-45, 2e-45, 3e-44, 1e-42, 7e-40, 1.17e-38, 1e-37, 1e-30):
+        check(s, where=str(s.scale))
+
+
 def test_weights_of_a_softmax_sum_to_one_a_row_and_head():
     """With attend's lse: every row and head gives one away."""
     from paper_2609_08450_amd import evict, paged
