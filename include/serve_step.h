@@ -80,8 +80,8 @@ size_t serve_weigh_workspace(int32_t n_rows, int32_t n_requests, int32_t heads, 
  * attention.  Tokens that no row sees, and those of a page outside the cache, keep
  * their weight.  A row with an lse of -inf (one that sees nothing) adds nothing.
  * FP32 products, exponentials and sums.
- *   q, act, table, row_starts, row_lengths, scale  as in paged_kv_attend; the cache
- *                   need not have values;
+ *   q, act, table, row_starts, row_lengths, scale  as in paged_kv_attend, scale below
+ *                   2.35e38; the cache need not have values;
  *   table_width     what the launch is laid out for, as the host knows no lengths: a table far
  *                   wider than the longest request costs time;
  *   lse             FP32 [n_rows][heads];

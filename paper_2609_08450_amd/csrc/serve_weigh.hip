@@ -973,6 +973,8 @@ extern "C" int serve_weigh(const paged_kv_cache *cache, int32_t act, const void 
         heads % cache->n_heads != 0 || table_width < 1 || table_stride < table_width || !(scale >= 0.0f) ||
         scale - scale != 0.0f)
         return PAGED_KV_EINVAL;
+    // (products are scaled by scale * log2(e))
+    if ((double)scale * 1.4426950408889634 > FLT_MAX) return PAGED_KV_EUNSUPPORTED;
     if (n_rows == 0 || n_requests == 0) return PAGED_KV_OK;
     const bool block = many(n_rows, n_requests, heads);
     if (!q || !lse || !table || !row_starts || !row_lengths || !weights || !weight_offsets || !aligned16(q) ||

@@ -145,6 +145,14 @@ def test_weigh_refusals(serve):
         assert L.serve_weigh_workspace(*sizes) == 0
 
 
+def test_scales_past_what_products_are_scaled_by(serve):
+    """log2(e) times the scale has to be an FP32 number, too."""
+    largest = torch.finfo(torch.float32).max
+    for scale in (largest, 2.4e38):
+        assert weigh(serve, scale=scale) == EUNSUPPORTED and weigh(serve, scale=scale, rows=0) == EUNSUPPORTED
+    assert weigh(serve, scale=2.35e38, rows=0) == 0
+
+
 def keep(serve, idx=P, K=5, base=0, lens=P, n=3, first=1, last=2, kept=12288, width=8, counts=8192, w=None, offsets=None):
     return serve.lib().serve_keep(idx, K, base, lens, n, first, last, kept, width, counts, w, offsets, None)
 
